@@ -58,7 +58,7 @@ enum {
     LLVQ_ETIMEOUT = 6       /* a bounded device-side wait ran out (flag in llvq_last_error) */
 };
 enum { LLVQ_LAYOUT_FLAT = 0, LLVQ_LAYOUT_ROWWISE = 1 };
-enum { LLVQ_F32 = 0, LLVQ_BF16 = 1 };
+enum { LLVQ_F32 = 0, LLVQ_BF16 = 1, LLVQ_F16 = 2 };
 enum { LLVQ_FLAG_WAIT_TIMEOUT = 1u,     /* bits in llvq_last_error's flags */
        LLVQ_FLAG_SEARCH_GAVE_UP = 4u }; /* the encoder's search found no point of the code for some input (non-finite input) */
 enum { LLVQ_EUCLIDEAN = 0, LLVQ_ANGULAR = 1 };   /* scoring of the encoder's search (Sec. 3.1) */
@@ -398,6 +398,74 @@ int llvq_exchange_close(const llvq_ctx* ctx, void* d_peer_buf);
 int llvq_signal_ranks(const llvq_ctx* ctx, uint32_t* const* d_flag_words, int n, uint32_t epoch, void* stream);
 int llvq_wait_ranks(const llvq_ctx* ctx, const uint32_t* d_flags, int world, int skip, uint32_t epoch,
                     uint32_t max_spins, void* stream);
+
+/*
+ * Layers that do not stand two bits (an output head, an embedding, a first or last layer) in microscaled 4-bit floating
+ * point (the OCP MX format with e2m1 elements), beside the lattice code.  None of these calls uses the context's code:
+ * any context of the device serves, for its error words.
+ *
+ * A rows x cols matrix is two arrays of bytes.  Codes: [rows][llvq_mx_code_pitch(cols)], 16 bytes per block of 32 columns,
+ * element 2i of a block in the low four bits of byte i, element 2i + 1 in the high four; an element is a sign bit and the
+ * three bits of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Elements past the last column are zero.  Scales:
+ * [rows][llvq_mx_scale_pitch(cols)], one byte e per block, the value 2^(e - 127), 255 = the block is NaN; a row is padded to a
+ * multiple of 16 bytes, and what the padding holds does not matter.  Both arrays are 16-byte aligned.  A band of whole rows
+ * of either array is the band of the matrix.  The pitches are 0 for cols < 0.
+ */
+int64_t llvq_mx_code_pitch(int64_t cols);
+int64_t llvq_mx_scale_pitch(int64_t cols);
+
+/* The CUDA device of a context; -1 for a host-only one (or NULL). */
+int llvq_device(const llvq_ctx* ctx);
+
+/*
+ * Quantisation.  Per block: e = floor(log2(largest magnitude)) - 2 + 127, at least 0; elements x / 2^(e - 127) to the nearest,
+ * ties to the even code, at most 6 in magnitude.  A block of zeros gets e = 0; one with an infinity or a NaN e = 255 and
+ * codes 0.  d_x: rows x cols of x_dtype (LLVQ_F32, LLVQ_BF16 or LLVQ_F16), leading dimension ld >= cols, aligned to its
+ * elements (16-byte aligned rows select wide loads).  Padding bytes of the scales are written as zero.
+ */
+int llvq_mx_quantize(const llvq_ctx* ctx, const void* d_x, int x_dtype, int64_t rows, int64_t cols, int64_t ld,
+                     uint8_t* d_codes, uint8_t* d_scales, void* stream);
+
+/* d_w[r*ld + c] = element * 2^(e - 127) as bf16 (exact, but for scales at the very top of the range, where it overflows to
+ * infinity).  d_w_bf16: leading dimension ld >= cols, 2-byte aligned. */
+int llvq_mx_dequant_matrix(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t rows, int64_t cols,
+                           uint16_t* d_w_bf16, int64_t ld, void* stream);
+
+/*
+ * y = W x and Y[b][i] = sum_k X[b][k] W[i][k] (batch <= 64) with W (n_out x k_in) in 4 bits and bf16 activations; the weights are the
+ * bf16 values of llvq_mx_dequant_matrix, products are accumulated in binary32, in an order that the sizes alone fix.
+ * d_x_bf16: [batch][k_in], 2-byte aligned, any k_in (rows on 16-byte boundaries are read fastest).  d_y: [n_out] float or bf16
+ * bits; d_y_bf16: [batch][n_out] bf16 bits.
+ */
+int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in,
+                 const uint16_t* d_x_bf16, void* d_y, int y_dtype, void* stream);
+int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in,
+                             const uint16_t* d_x_bf16, int batch, uint16_t* d_y_bf16, void* stream);
+
+/*
+ * Rows of a table by token: d_out[i][c] = scale * table[d_tokens[i]][c], one multiplication in binary32 and one rounding to the
+ * output's type (bf16 for a table in 4 bits, else the table's).  d_table: [vocab][dim] of dtype; d_tokens: [n] of int32
+ * (token_bytes = 4) or int64 (8); d_out: [n][dim].  All aligned to their elements.  A token outside [0, vocab) gives a row of
+ * zeros and is counted like an out-of-range index (llvq_last_error).
+ */
+int llvq_embed(const llvq_ctx* ctx, const void* d_table, int dtype, int64_t vocab, int64_t dim, const void* d_tokens,
+               int token_bytes, int64_t n, float scale, void* d_out, void* stream);
+int llvq_mx_embed(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t vocab, int64_t dim,
+                  const void* d_tokens, int token_bytes, int64_t n, float scale, uint16_t* d_out_bf16, void* stream);
+
+/*
+ * The gradient of llvq_embed with respect to its table: d_grad[v][c] = scale * sum of d_dy[i][c] over the i with token v (plus what
+ * d_grad held, with accumulate != 0), summed in binary32 in an order that the tokens alone fix (two calls on the same inputs
+ * agree to the bit), rounded once.  Tokens equal to padding_idx contribute nothing (-1: no such row; a token of -1 is then left
+ * out); other tokens outside [0, vocab) contribute nothing and are counted.  Every row of d_grad is written unless accumulate is set.
+ * d_dy: [n][dim] of dy_dtype; d_grad: [vocab][dim] of grad_dtype; any of the three types each.  d_work: 256-byte aligned device
+ * memory of llvq_embed_grad_bytes(n, dim) bytes (0: sizes that are not supported, or nothing to do), which belongs to the call
+ * until it is done: calls that may overlap need one each.
+ */
+size_t llvq_embed_grad_bytes(int64_t n, int64_t dim);
+int llvq_embed_grad(const llvq_ctx* ctx, const void* d_dy, int dy_dtype, const void* d_tokens, int token_bytes, int64_t n,
+                    int64_t vocab, int64_t dim, float scale, int64_t padding_idx, int accumulate, void* d_grad, int grad_dtype,
+                    void* d_work, void* stream);
 
 /*
  * Self-test of the error path every kernel of this library uses for its device-side waits (table copy,

@@ -29,11 +29,13 @@ __all__ = [
     "llvq_gemm_small_batch_rowshard", "llvq_gemm_small_batch_sorted_rowshard",
     "llvq_sort_blocks_gemm_sg", "llvq_gemm_small_batch_sorted_sg",
     "llvq_last_error", "LlvqError", "EXPORTS", "load_library", "llvq_gemv_multi", "llvq_gemv_sorted_multi", "GemvDesc",
-    "LLVQ_LAYOUT_FLAT", "LLVQ_LAYOUT_ROWWISE", "LLVQ_F32", "LLVQ_BF16",
+    "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch", "llvq_mx_code_pitch", "llvq_mx_scale_pitch",
+    "llvq_embed", "llvq_mx_embed", "llvq_embed_grad",
+    "LLVQ_LAYOUT_FLAT", "LLVQ_LAYOUT_ROWWISE", "LLVQ_F32", "LLVQ_BF16", "LLVQ_F16",
 ]
 
 LLVQ_LAYOUT_FLAT, LLVQ_LAYOUT_ROWWISE = 0, 1
-LLVQ_F32, LLVQ_BF16 = 0, 1
+LLVQ_F32, LLVQ_BF16, LLVQ_F16 = 0, 1, 2
 LLVQ_EUCLIDEAN, LLVQ_ANGULAR = 0, 1
 LLVQ_FLAG_WAIT_TIMEOUT, LLVQ_FLAG_SEARCH_GAVE_UP = 1, 4
 LLVQ_EXCHANGE_HANDLE_BYTES = 64
@@ -54,6 +56,8 @@ EXPORTS = [
     "llvq_gemm_small_batch_rowshard", "llvq_gemm_small_batch_sorted_rowshard",
     "llvq_sort_blocks_gemm_sg", "llvq_gemm_small_batch_sorted_sg",
     "llvq_gemv_multi", "llvq_gemv_sorted_multi",
+    "llvq_device", "llvq_mx_code_pitch", "llvq_mx_scale_pitch", "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch",
+    "llvq_embed", "llvq_mx_embed", "llvq_embed_grad_bytes", "llvq_embed_grad",
 ]
 
 
@@ -125,6 +129,20 @@ def load_library() -> ctypes.CDLL:
     lib.llvq_last_error.argtypes = [vp, vp, ctypes.POINTER(u64), ctypes.POINTER(ctypes.c_uint32)]
     lib.llvq_class_info.argtypes = [vp, ctypes.c_int, vp, vp, vp, vp, vp, vp]
     lib.llvq_golay_table.argtypes = [vp, vp]
+    lib.llvq_device.argtypes = [vp]
+    lib.llvq_mx_code_pitch.argtypes = [i64]
+    lib.llvq_mx_code_pitch.restype = i64
+    lib.llvq_mx_scale_pitch.argtypes = [i64]
+    lib.llvq_mx_scale_pitch.restype = i64
+    lib.llvq_mx_quantize.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, vp, vp, vp]
+    lib.llvq_mx_dequant_matrix.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp]
+    lib.llvq_mx_gemv.argtypes = [vp, vp, vp, i64, i64, vp, vp, ctypes.c_int, vp]
+    lib.llvq_mx_gemm_small_batch.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp]
+    lib.llvq_embed.argtypes = [vp, vp, ctypes.c_int, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]
+    lib.llvq_mx_embed.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]
+    lib.llvq_embed_grad_bytes.argtypes = [i64, i64]
+    lib.llvq_embed_grad_bytes.restype = ctypes.c_size_t
+    lib.llvq_embed_grad.argtypes = [vp, vp, ctypes.c_int, vp, ctypes.c_int, i64, i64, i64, ctypes.c_float, i64, ctypes.c_int, vp, ctypes.c_int, vp, vp]
     shard = [vp, vp, vp, i64, i64, vp, ctypes.POINTER(vp), ctypes.c_int, ctypes.c_int, i64, ctypes.c_int, ctypes.POINTER(vp),
              ctypes.c_uint32, vp]
     lib.llvq_gemv_rowshard.argtypes = shard
@@ -399,6 +417,61 @@ def llvq_pack_fields(ctx: Context, d_index: torch.Tensor, d_gain_index: torch.Te
                      d_fields: torch.Tensor | None = None, stream=None):
     """The stored stream (uint8) of the fields index | gain index << index_bits."""
     return _out("llvq_pack_fields", _native.pack(ctx._ptr, d_index, d_gain_index, gain_bits, d_fields, _stream_arg(stream)))
+
+
+def llvq_mx_code_pitch(cols: int) -> int:
+    """Bytes of a row of 4-bit codes: 16 per block of 32 columns."""
+    return int(load_library().llvq_mx_code_pitch(cols))
+
+
+def llvq_mx_scale_pitch(cols: int) -> int:
+    """Bytes of a row of scales: one per block of 32 columns, rounded up to 16."""
+    return int(load_library().llvq_mx_scale_pitch(cols))
+
+
+def llvq_mx_quantize(ctx: Context, d_x: torch.Tensor, d_codes: torch.Tensor | None = None, d_scales: torch.Tensor | None = None, stream=None):
+    """(codes, scales), uint8 [rows, code pitch] and [rows, scale pitch], of the matrix ``d_x`` (float32, bfloat16 or float16 [rows, cols], rows
+    contiguous) in microscaled 4-bit floating point: blocks of 32 columns that share a power of two."""
+    return _out("llvq_mx_quantize", _native.mx_quantize(ctx._ptr, d_x, d_codes, d_scales, _stream_arg(stream)))
+
+
+def llvq_mx_dequant_matrix(ctx: Context, d_codes: torch.Tensor, d_scales: torch.Tensor, rows: int, cols: int, d_w: torch.Tensor | None = None,
+                           ld: int | None = None, stream=None):
+    """bf16 [rows, cols] values of a matrix made by ``llvq_mx_quantize``."""
+    return _out("llvq_mx_dequant_matrix", _native.mx_dequant(ctx._ptr, d_codes, d_scales, rows, cols, d_w, cols if ld is None else ld, _stream_arg(stream)))
+
+
+def llvq_mx_gemv(ctx: Context, d_codes: torch.Tensor, d_scales: torch.Tensor, n_out: int, k_in: int, d_x: torch.Tensor,
+                 d_y: torch.Tensor | None = None, y_dtype: torch.dtype = torch.float32, stream=None):
+    """y = W x with W (n_out x k_in) in 4 bits; x bf16 [k_in]; y float32 or bf16 [n_out]."""
+    return _out("llvq_mx_gemv", _native.mx_gemv(ctx._ptr, d_codes, d_scales, n_out, k_in, d_x, d_y, y_dtype, _stream_arg(stream)))
+
+
+def llvq_mx_gemm_small_batch(ctx: Context, d_codes: torch.Tensor, d_scales: torch.Tensor, n_out: int, k_in: int, d_x: torch.Tensor,
+                             d_y: torch.Tensor | None = None, stream=None):
+    """Y[b, i] = sum_k X[b, k] W[i, k] with W in 4 bits; X bf16 [batch, k_in], Y bf16 [batch, n_out], batch <= 64."""
+    return _out("llvq_mx_gemm_small_batch", _native.mx_gemm_small(ctx._ptr, d_codes, d_scales, n_out, k_in, d_x, d_y, _stream_arg(stream)))
+
+
+def llvq_embed(ctx: Context, d_table: torch.Tensor, d_tokens: torch.Tensor, scale: float = 1.0, d_out: torch.Tensor | None = None, stream=None):
+    """scale * table[tokens]: ``d_table`` float32, bfloat16 or float16 [vocab, dim], ``d_tokens`` int32 or int64 of any shape, the result
+    [*tokens.shape, dim] of the table's type.  A token outside the table gives zeros and is counted (``llvq_last_error``)."""
+    return _out("llvq_embed", _native.embed(ctx._ptr, d_table, d_tokens, scale, d_out, _stream_arg(stream)))
+
+
+def llvq_mx_embed(ctx: Context, d_codes: torch.Tensor, d_scales: torch.Tensor, vocab: int, dim: int, d_tokens: torch.Tensor, scale: float = 1.0,
+                  d_out: torch.Tensor | None = None, stream=None):
+    """``llvq_embed`` from a table in 4 bits (``llvq_mx_quantize``); the result is bf16."""
+    return _out("llvq_mx_embed", _native.mx_embed(ctx._ptr, d_codes, d_scales, vocab, dim, d_tokens, scale, d_out, _stream_arg(stream)))
+
+
+def llvq_embed_grad(ctx: Context, d_dy: torch.Tensor, d_tokens: torch.Tensor, vocab: int, scale: float = 1.0, padding_idx: int = -1,
+                    d_grad: torch.Tensor | None = None, grad_dtype: torch.dtype = torch.float32, accumulate: bool = False, stream=None):
+    """Gradient [vocab, dim] of ``llvq_embed`` with respect to its table: row v is scale times the sum of the rows of ``d_dy``
+    ([*tokens.shape, dim]) whose token is v, in binary32 and in an order that the tokens alone fix; tokens equal to ``padding_idx`` are left
+    out.  With ``accumulate`` it is added to ``d_grad``."""
+    return _out("llvq_embed_grad", _native.embed_grad(ctx._ptr, d_dy, d_tokens, vocab, scale, padding_idx, d_grad, grad_dtype, bool(accumulate),
+                                                      _stream_arg(stream)))
 
 
 def _ptr(p, name: str) -> int:

@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include "llvq.h"
@@ -406,10 +407,233 @@ LLVQ_FUNC(pack, 6)
     return result(s, std::move(f));
 }
 
+// ---- microscaled 4-bit floating point, embedding tables --------------------------------------------------------------------------
+
+// The stream that the call is given, or PyTorch's current one of the device that `t` is on.
+void* stream_of(Args& A, int i, const at::Tensor& t)
+{
+    if (!A.ok) return nullptr;
+    if (A.a[i] == Py_None && t.is_cuda()) return c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
+    return A.stream(i);
+}
+
+// The tensor's memory, on the context's device.
+void* on_device(Args& A, const llvq_ctx* ctx, const at::Tensor* t, const char* name)
+{
+    void* p = A.device(t, name);
+    if (A.ok && t && llvq_device(ctx) >= 0) A.expect(t->device().index() == llvq_device(ctx));
+    return A.ok ? p : nullptr;
+}
+
+// LLVQ_F32, LLVQ_BF16 or LLVQ_F16; -1 for other types
+int float_code(at::ScalarType t) { return t == at::kFloat ? LLVQ_F32 : t == at::kBFloat16 ? LLVQ_BF16 : t == at::kHalf ? LLVQ_F16 : -1; }
+
+struct Mx { const uint8_t *codes, *scales; };
+// A rows x cols matrix in 4 bits
+Mx mx_args(Args& A, const llvq_ctx* ctx, const at::Tensor* codes, const at::Tensor* scales, int64_t rows, int64_t cols)
+{
+    if (!A.expect(rows >= 0 && cols >= 0 && codes->scalar_type() == at::kByte && scales->scalar_type() == at::kByte)) return {};
+    A.expect((__int128)codes->numel() >= (__int128)rows * llvq_mx_code_pitch(cols) && (__int128)scales->numel() >= (__int128)rows * llvq_mx_scale_pitch(cols));
+    const uint8_t* c = static_cast<const uint8_t*>(on_device(A, ctx, codes, "d_codes"));
+    return {c, static_cast<const uint8_t*>(on_device(A, ctx, scales, "d_scales"))};
+}
+
+// tokens of an embedding, and how many bytes one has
+const void* token_args(Args& A, const llvq_ctx* ctx, const at::Tensor* t, int* bytes)
+{
+    A.expect(t->scalar_type() == at::kLong || t->scalar_type() == at::kInt);
+    *bytes = t->scalar_type() == at::kLong ? 8 : 4;
+    return on_device(A, ctx, t, "d_tokens");
+}
+
+double real(Args& A, int i)
+{
+    if (!A.ok) return 0.0;
+    const double v = PyFloat_AsDouble(A.a[i]);
+    if (v == -1.0 && PyErr_Occurred()) A.ok = false;
+    return v;
+}
+
+PyObject* pair(at::Tensor&& x, at::Tensor&& y, bool* ok)
+{
+    PyObject *a = THPVariable_Wrap(std::move(x)), *b = THPVariable_Wrap(std::move(y));
+    PyObject* r = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+    Py_XDECREF(a);
+    Py_XDECREF(b);
+    if (!r) *ok = false;
+    return r;
+}
+
+// (ctx, x, codes or None, scales or None, stream) -> (codes, scales); rows of x may be further apart than they are long
+LLVQ_FUNC(mx_quantize, 5)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *x = A.tensor(1, "d_x"), *c0 = A.tensor_or_none(2, "d_codes"), *s0 = A.tensor_or_none(3, "d_scales");
+    if (!A.ok) return nullptr;
+    const int type = float_code(x->scalar_type());
+    if (!A.expect(type >= 0 && x->dim() == 2)) return nullptr;
+    const int64_t rows = x->size(0), cols = x->size(1), ld = rows > 1 ? x->stride(0) : cols;
+    if (!x->is_cuda()) { A.wrong("d_x"); return nullptr; }
+    if (!A.expect((cols <= 1 || x->stride(1) == 1) && ld >= cols)) return nullptr;
+    if (llvq_device(ctx) >= 0 && !A.expect(x->device().index() == llvq_device(ctx))) return nullptr;
+    at::Tensor c = c0 ? *c0 : new_tensor({rows, llvq_mx_code_pitch(cols)}, at::kByte, *x), s = s0 ? *s0 : new_tensor({rows, llvq_mx_scale_pitch(cols)}, at::kByte, *x);
+    const Mx m = mx_args(A, ctx, &c, &s, rows, cols);
+    void* st = stream_of(A, 4, *x);
+    if (!A.ok) return nullptr;
+    const void* px = x->data_ptr();
+    const int r = call([&] { return llvq_mx_quantize(ctx, px, type, rows, cols, ld, const_cast<uint8_t*>(m.codes), const_cast<uint8_t*>(m.scales), st); });
+    if (r != LLVQ_OK) return PyLong_FromLong(r);
+    return pair(std::move(c), std::move(s), &A.ok);
+}
+
+// (ctx, codes, scales, rows, cols, W or None, ld, stream)
+LLVQ_FUNC(mx_dequant, 8)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *c = A.tensor(1, "d_codes"), *s = A.tensor(2, "d_scales"), *w0 = A.tensor_or_none(5, "d_w");
+    const int64_t rows = A.integer(3), cols = A.integer(4), ld = A.integer(6);
+    if (!A.ok) return nullptr;
+    if (!A.expect(rows >= 0 && cols >= 0 && ld >= cols)) return nullptr;
+    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *c);
+    A.expect(w.scalar_type() == at::kBFloat16);
+    A.expect(holds(w, rows, cols, ld));
+    if (!A.ok) return nullptr;
+    const Mx m = mx_args(A, ctx, c, s, rows, cols);
+    uint16_t* pw = static_cast<uint16_t*>(on_device(A, ctx, &w, "d_w"));
+    void* st = stream_of(A, 7, *c);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_mx_dequant_matrix(ctx, m.codes, m.scales, rows, cols, pw, ld, st); });
+    return result(r, std::move(w));
+}
+
+// (ctx, codes, scales, n_out, k_in, x, y or None, y_dtype, stream)
+LLVQ_FUNC(mx_gemv, 9)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *c = A.tensor(1, "d_codes"), *s = A.tensor(2, "d_scales"), *x = A.tensor(5, "d_x"), *y0 = A.tensor_or_none(6, "d_y");
+    const int64_t n_out = A.integer(3), k_in = A.integer(4);
+    if (!A.ok) return nullptr;
+    const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(7);
+    if (!A.expect(n_out >= 0 && (yt == at::kFloat || yt == at::kBFloat16))) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *c);
+    A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in && y.numel() >= n_out);
+    if (!A.ok) return nullptr;
+    const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
+    const uint16_t* px = static_cast<const uint16_t*>(on_device(A, ctx, x, "d_x"));
+    void *py = on_device(A, ctx, &y, "d_y"), *st = stream_of(A, 8, *c);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_mx_gemv(ctx, m.codes, m.scales, n_out, k_in, px, py, y_code(yt), st); });
+    return result(r, std::move(y));
+}
+
+// (ctx, codes, scales, n_out, k_in, X, Y or None, stream)
+LLVQ_FUNC(mx_gemm_small, 8)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *c = A.tensor(1, "d_codes"), *s = A.tensor(2, "d_scales"), *x = A.tensor(5, "d_x"), *y0 = A.tensor_or_none(6, "d_y");
+    const int64_t n_out = A.integer(3), k_in = A.integer(4);
+    if (!A.ok) return nullptr;
+    if (!A.expect(n_out >= 0 && x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in)) return nullptr;
+    const int64_t batch = x->size(0);
+    if (batch > 64) return PyLong_FromLong(LLVQ_EUNSUPPORTED);
+    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *c);
+    A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)batch * n_out);
+    if (!A.ok) return nullptr;
+    const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
+    const uint16_t* px = static_cast<const uint16_t*>(on_device(A, ctx, x, "d_x"));
+    uint16_t* py = static_cast<uint16_t*>(on_device(A, ctx, &y, "d_y"));
+    void* st = stream_of(A, 7, *c);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_mx_gemm_small_batch(ctx, m.codes, m.scales, n_out, k_in, px, (int)batch, py, st); });
+    return result(r, std::move(y));
+}
+
+at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type)
+{
+    std::vector<int64_t> shape(tokens.sizes().begin(), tokens.sizes().end());
+    shape.push_back(dim);
+    return new_tensor(shape, type, tokens);
+}
+
+// (ctx, table, tokens, scale, out or None, stream)
+LLVQ_FUNC(embed, 6)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *w = A.tensor(1, "d_table"), *t = A.tensor(2, "d_tokens"), *o0 = A.tensor_or_none(4, "d_out");
+    const double scale = real(A, 3);
+    if (!A.ok) return nullptr;
+    const int type = float_code(w->scalar_type());
+    if (!A.expect(type >= 0 && w->dim() == 2)) return nullptr;
+    const int64_t n = t->numel(), dim = w->size(1);
+    at::Tensor o = o0 ? *o0 : embedded(*t, dim, w->scalar_type());
+    if (!A.expect(o.scalar_type() == w->scalar_type() && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
+    int bytes;
+    const void *pt = token_args(A, ctx, t, &bytes), *pw = on_device(A, ctx, w, "d_table");
+    void *po = on_device(A, ctx, &o, "d_out"), *st = stream_of(A, 5, *w);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_embed(ctx, pw, type, w->size(0), dim, pt, bytes, n, (float)scale, po, st); });
+    return result(r, std::move(o));
+}
+
+// (ctx, codes, scales, vocab, dim, tokens, scale, out or None, stream)
+LLVQ_FUNC(mx_embed, 9)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *c = A.tensor(1, "d_codes"), *s = A.tensor(2, "d_scales"), *t = A.tensor(5, "d_tokens"), *o0 = A.tensor_or_none(7, "d_out");
+    const int64_t vocab = A.integer(3), dim = A.integer(4);
+    const double scale = real(A, 6);
+    if (!A.ok) return nullptr;
+    if (!A.expect(dim >= 0)) return nullptr;
+    const int64_t n = t->numel();
+    at::Tensor o = o0 ? *o0 : embedded(*t, dim, at::kBFloat16);
+    if (!A.expect(o.scalar_type() == at::kBFloat16 && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
+    const Mx m = mx_args(A, ctx, c, s, vocab, dim);
+    if (!A.ok) return nullptr;
+    int bytes;
+    const void* pt = token_args(A, ctx, t, &bytes);
+    uint16_t* po = static_cast<uint16_t*>(on_device(A, ctx, &o, "d_out"));
+    void* st = stream_of(A, 8, *c);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_mx_embed(ctx, m.codes, m.scales, vocab, dim, pt, bytes, n, (float)scale, po, st); });
+    return result(r, std::move(o));
+}
+
+// (ctx, dy, tokens, vocab, scale, padding_idx, grad or None, grad_dtype, accumulate, stream)
+LLVQ_FUNC(embed_grad, 10)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *dy = A.tensor(1, "d_dy"), *t = A.tensor(2, "d_tokens"), *g0 = A.tensor_or_none(6, "d_grad");
+    const int64_t vocab = A.integer(3), padding = A.integer(5);
+    const double scale = real(A, 4);
+    const bool accumulate = A.a[8] == Py_True;
+    if (!A.ok) return nullptr;
+    const at::ScalarType gt = g0 ? g0->scalar_type() : A.dtype(7);
+    if (!A.ok) return nullptr;
+    const int type = float_code(dy->scalar_type()), grad_type = float_code(gt);
+    if (!A.expect(type >= 0 && grad_type >= 0 && vocab >= 0 && dy->dim() >= 1 && (!accumulate || g0))) return nullptr;
+    const int64_t n = t->numel(), dim = dy->size(-1);
+    if (!A.expect((__int128)dy->numel() == (__int128)n * dim)) return nullptr;
+    at::Tensor g = g0 ? *g0 : new_tensor({vocab, dim}, gt, *dy);
+    if (!A.expect((__int128)g.numel() >= (__int128)vocab * dim)) return nullptr;
+    int bytes;
+    const void *pt = token_args(A, ctx, t, &bytes), *pd = on_device(A, ctx, dy, "d_dy");
+    void *pg = on_device(A, ctx, &g, "d_grad"), *st = stream_of(A, 9, *dy);
+    if (!A.ok) return nullptr;
+    // The call's own lists and sums, from PyTorch's allocator: on a stream that is not the current one the memory is marked as in use there.
+    const at::Tensor work = new_tensor({(int64_t)llvq_embed_grad_bytes(n, dim)}, at::kByte, *dy);
+    if (A.a[9] != Py_None && work.numel() > 0)
+        c10::cuda::CUDACachingAllocator::recordStream(work.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), dy->device().index()));
+    const int r = call([&] {
+        return llvq_embed_grad(ctx, pd, type, pt, bytes, n, vocab, dim, (float)scale, padding, accumulate, pg, grad_type, work.numel() ? work.data_ptr() : nullptr, st);
+    });
+    return result(r, std::move(g));
+}
+
 #define LLVQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LLVQ_METHOD(gemv), LLVQ_METHOD(gemv_sg), LLVQ_METHOD(gemm), LLVQ_METHOD(gemm_sg), LLVQ_METHOD(gemv_multi),
                          LLVQ_METHOD(dequant), LLVQ_METHOD(dequant_sg), LLVQ_METHOD(decode), LLVQ_METHOD(encode), LLVQ_METHOD(rank),
-                         LLVQ_METHOD(pack), {nullptr, nullptr, 0, nullptr}};
+                         LLVQ_METHOD(pack), LLVQ_METHOD(mx_quantize), LLVQ_METHOD(mx_dequant), LLVQ_METHOD(mx_gemv), LLVQ_METHOD(mx_gemm_small),
+                         LLVQ_METHOD(embed), LLVQ_METHOD(mx_embed), LLVQ_METHOD(embed_grad), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Entry points of libllvq.so on PyTorch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
