@@ -443,6 +443,14 @@ int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const 
                              const uint16_t* d_x_bf16, int batch, uint16_t* d_y_bf16, void* stream);
 
 /*
+ * Y[t][i] = sum_k X[t][k] W[i][k] with both operands in 4 bits (a prompt's activations by llvq_mx_quantize, any number of tokens) on the
+ * tensor cores' block-scaled instruction: products of the stored values, binary32 sums, one rounding to bf16.  d_x_codes / d_x_scales:
+ * tokens x k_in; d_codes / d_scales: n_out x k_in; d_y_bf16: [tokens][n_out], 2-byte aligned.  Sizes up to 2^30 each.
+ */
+int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const uint8_t* d_x_scales, int64_t tokens, const uint8_t* d_codes,
+                 const uint8_t* d_scales, int64_t n_out, int64_t k_in, uint16_t* d_y_bf16, void* stream);
+
+/*
  * Rows of a table by token: d_out[i][c] = scale * table[d_tokens[i]][c], one multiplication in binary32 and one rounding to the
  * output's type (bf16 for a table in 4 bits, else the table's).  d_table: [vocab][dim] of dtype; d_tokens: [n] of int32
  * (token_bytes = 4) or int64 (8); d_out: [n][dim].  All aligned to their elements.  A token outside [0, vocab) gives a row of

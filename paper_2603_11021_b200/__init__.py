@@ -29,7 +29,7 @@ __all__ = [
     "llvq_gemm_small_batch_rowshard", "llvq_gemm_small_batch_sorted_rowshard",
     "llvq_sort_blocks_gemm_sg", "llvq_gemm_small_batch_sorted_sg",
     "llvq_last_error", "LlvqError", "EXPORTS", "load_library", "llvq_gemv_multi", "llvq_gemv_sorted_multi", "GemvDesc",
-    "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch", "llvq_mx_code_pitch", "llvq_mx_scale_pitch",
+    "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch", "llvq_mx_gemm", "llvq_mx_code_pitch", "llvq_mx_scale_pitch",
     "llvq_embed", "llvq_mx_embed", "llvq_embed_grad",
     "LLVQ_LAYOUT_FLAT", "LLVQ_LAYOUT_ROWWISE", "LLVQ_F32", "LLVQ_BF16", "LLVQ_F16",
 ]
@@ -57,7 +57,7 @@ EXPORTS = [
     "llvq_sort_blocks_gemm_sg", "llvq_gemm_small_batch_sorted_sg",
     "llvq_gemv_multi", "llvq_gemv_sorted_multi",
     "llvq_device", "llvq_mx_code_pitch", "llvq_mx_scale_pitch", "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch",
-    "llvq_embed", "llvq_mx_embed", "llvq_embed_grad_bytes", "llvq_embed_grad",
+    "llvq_mx_gemm", "llvq_embed", "llvq_mx_embed", "llvq_embed_grad_bytes", "llvq_embed_grad",
 ]
 
 
@@ -138,6 +138,7 @@ def load_library() -> ctypes.CDLL:
     lib.llvq_mx_dequant_matrix.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp]
     lib.llvq_mx_gemv.argtypes = [vp, vp, vp, i64, i64, vp, vp, ctypes.c_int, vp]
     lib.llvq_mx_gemm_small_batch.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp]
+    lib.llvq_mx_gemm.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, vp, vp]
     lib.llvq_embed.argtypes = [vp, vp, ctypes.c_int, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]
     lib.llvq_mx_embed.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]
     lib.llvq_embed_grad_bytes.argtypes = [i64, i64]
@@ -451,6 +452,12 @@ def llvq_mx_gemm_small_batch(ctx: Context, d_codes: torch.Tensor, d_scales: torc
                              d_y: torch.Tensor | None = None, stream=None):
     """Y[b, i] = sum_k X[b, k] W[i, k] with W in 4 bits; X bf16 [batch, k_in], Y bf16 [batch, n_out], batch <= 64."""
     return _out("llvq_mx_gemm_small_batch", _native.mx_gemm_small(ctx._ptr, d_codes, d_scales, n_out, k_in, d_x, d_y, _stream_arg(stream)))
+
+
+def llvq_mx_gemm(ctx: Context, d_x_codes: torch.Tensor, d_x_scales: torch.Tensor, tokens: int, d_codes: torch.Tensor, d_scales: torch.Tensor, n_out: int,
+                 k_in: int, d_y: torch.Tensor | None = None, stream=None):
+    """Y[t, i] = sum_k X[t, k] W[i, k] with both operands in 4 bits (``llvq_mx_quantize``); Y bf16 [tokens, n_out]."""
+    return _out("llvq_mx_gemm", _native.mx_gemm(ctx._ptr, d_x_codes, d_x_scales, tokens, d_codes, d_scales, n_out, k_in, d_y, _stream_arg(stream)))
 
 
 def llvq_embed(ctx: Context, d_table: torch.Tensor, d_tokens: torch.Tensor, scale: float = 1.0, d_out: torch.Tensor | None = None, stream=None):

@@ -429,11 +429,15 @@ void* on_device(Args& A, const llvq_ctx* ctx, const at::Tensor* t, const char* n
 int float_code(at::ScalarType t) { return t == at::kFloat ? LLVQ_F32 : t == at::kBFloat16 ? LLVQ_BF16 : t == at::kHalf ? LLVQ_F16 : -1; }
 
 struct Mx { const uint8_t *codes, *scales; };
-// A rows x cols matrix in 4 bits
+// Whether codes and scales hold a rows x cols matrix in 4 bits
+bool mx_holds(const at::Tensor& codes, const at::Tensor& scales, int64_t rows, int64_t cols)
+{
+    return rows >= 0 && cols >= 0 && codes.scalar_type() == at::kByte && scales.scalar_type() == at::kByte &&
+           (__int128)codes.numel() >= (__int128)rows * llvq_mx_code_pitch(cols) && (__int128)scales.numel() >= (__int128)rows * llvq_mx_scale_pitch(cols);
+}
 Mx mx_args(Args& A, const llvq_ctx* ctx, const at::Tensor* codes, const at::Tensor* scales, int64_t rows, int64_t cols)
 {
-    if (!A.expect(rows >= 0 && cols >= 0 && codes->scalar_type() == at::kByte && scales->scalar_type() == at::kByte)) return {};
-    A.expect((__int128)codes->numel() >= (__int128)rows * llvq_mx_code_pitch(cols) && (__int128)scales->numel() >= (__int128)rows * llvq_mx_scale_pitch(cols));
+    if (!A.expect(mx_holds(*codes, *scales, rows, cols))) return {};
     const uint8_t* c = static_cast<const uint8_t*>(on_device(A, ctx, codes, "d_codes"));
     return {c, static_cast<const uint8_t*>(on_device(A, ctx, scales, "d_scales"))};
 }
@@ -548,6 +552,28 @@ LLVQ_FUNC(mx_gemm_small, 8)
     return result(r, std::move(y));
 }
 
+// (ctx, x codes, x scales, tokens, codes, scales, n_out, k_in, Y or None, stream)
+LLVQ_FUNC(mx_gemm, 10)
+{
+    const llvq_ctx* ctx = A.context(0);
+    const at::Tensor *xc = A.tensor(1, "d_x_codes"), *xs = A.tensor(2, "d_x_scales"), *c = A.tensor(4, "d_codes"), *s = A.tensor(5, "d_scales"),
+                     *y0 = A.tensor_or_none(8, "d_y");
+    const int64_t tokens = A.integer(3), n_out = A.integer(6), k_in = A.integer(7);
+    if (!A.ok) return nullptr;
+    if (!A.expect(mx_holds(*xc, *xs, tokens, k_in) && mx_holds(*c, *s, n_out, k_in))) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({tokens, n_out}, at::kBFloat16, *c);
+    A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)tokens * n_out);
+    if (!A.ok) return nullptr;
+    const Mx x = mx_args(A, ctx, xc, xs, tokens, k_in);
+    if (!A.ok) return nullptr;
+    const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
+    uint16_t* py = static_cast<uint16_t*>(on_device(A, ctx, &y, "d_y"));
+    void* st = stream_of(A, 9, *c);
+    if (!A.ok) return nullptr;
+    const int r = call([&] { return llvq_mx_gemm(ctx, x.codes, x.scales, tokens, m.codes, m.scales, n_out, k_in, py, st); });
+    return result(r, std::move(y));
+}
+
 at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type)
 {
     std::vector<int64_t> shape(tokens.sizes().begin(), tokens.sizes().end());
@@ -632,7 +658,7 @@ LLVQ_FUNC(embed_grad, 10)
 #define LLVQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LLVQ_METHOD(gemv), LLVQ_METHOD(gemv_sg), LLVQ_METHOD(gemm), LLVQ_METHOD(gemm_sg), LLVQ_METHOD(gemv_multi),
                          LLVQ_METHOD(dequant), LLVQ_METHOD(dequant_sg), LLVQ_METHOD(decode), LLVQ_METHOD(encode), LLVQ_METHOD(rank),
-                         LLVQ_METHOD(pack), LLVQ_METHOD(mx_quantize), LLVQ_METHOD(mx_dequant), LLVQ_METHOD(mx_gemv), LLVQ_METHOD(mx_gemm_small),
+                         LLVQ_METHOD(pack), LLVQ_METHOD(mx_quantize), LLVQ_METHOD(mx_dequant), LLVQ_METHOD(mx_gemv), LLVQ_METHOD(mx_gemm_small), LLVQ_METHOD(mx_gemm),
                          LLVQ_METHOD(embed), LLVQ_METHOD(mx_embed), LLVQ_METHOD(embed_grad), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Entry points of libllvq.so on PyTorch tensors.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

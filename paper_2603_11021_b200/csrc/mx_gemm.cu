@@ -1,0 +1,310 @@
+// Product of two matrices in microscaled 4-bit floating point on the tensor cores' own block-scaled instruction (see include/llvq.h and mx.cuh):
+// Y[t][i] = sum_k X[t][k] W[i][k], both operands as llvq_mx_quantize leaves them, sums in binary32, Y in bf16.
+#include "kernels_common.cuh"
+#include "mx.cuh"
+#include "umma.cuh"
+
+namespace {
+
+using namespace llvq;
+
+// tcgen05.mma.kind::mxf4 takes e2m1 operands from shared memory and one e8m0 scale per row and 32 columns from tensor memory: nothing of
+// either operand passes through registers.  A thread block computes tiles of 128 rows of W (the lanes of tensor memory) by kBn tokens
+// (its columns), 256 columns of both operands (128 bytes of codes per row) per stage:
+//   warp 0      copies codes with TMA (swizzled rows of 128 bytes; what lies past the matrix reads as zero)
+//   warps 2, 3  lay the scales of W and X out as tcgen05.cp wants them: of 128 rows and 4 blocks, 512 bytes, row r at 16 (r % 32) + 4 (r / 32).
+//               A lane loads 16 scales of four rows 32 apart (16 bytes each: that is what the rows' padding is for) and stores four times 16 bytes
+//   warp 1      copies the scales to tensor memory and issues four MMAs of 64 columns per stage
+//   warps 4-11  take the accumulator out as bf16 (a quarter of the lanes by half of the columns each), hand it back, then write Y
+// There is one accumulator: taking it out costs the tensor cores a few hundred of the thousands of cycles of a tile.
+constexpr int kMmThreads = 384;
+constexpr int kMmRows = 128;                              // rows of W per tile
+constexpr int kMmGroup = 16;                              // row tiles that are walked together, for L2
+constexpr uint32_t kStageCodes = 128;                     // bytes of a row's codes per stage: 256 columns
+constexpr uint32_t kScaleAtom = 512;                      // scales of 128 rows and 4 blocks
+
+template <int kBn> struct MmShape {
+    static constexpr int kBHalves = kBn > 128 ? 2 : 1;    // groups of 128 tokens
+    static constexpr uint32_t kA = kMmRows * kStageCodes, kB = kBn * kStageCodes, kScales = (2 + 2 * kBHalves) * kScaleAtom;
+    static constexpr uint32_t kStage = kA + kB + kScales; // a multiple of 1024
+    static constexpr int kStages = kBn == 256 ? 4 : kBn == 128 ? 6 : 8;
+    static constexpr uint32_t kScaleCols = 8 + 8 * kBHalves;      // columns of tensor memory that a stage's scales take
+    static constexpr uint32_t kTmem = kBn == 256 ? 512 : kBn == 128 ? 256 : 128;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 256;
+    static_assert(kStage % 1024 == 0 && kBn + 2 * kScaleCols <= kTmem && kSmem <= 227 * 1024, "");
+};
+
+struct MmArgs {
+    const uint8_t *w_scales, *x_scales;
+    int64_t n_out, tokens;
+    uint32_t kb, pitch, k_stages;                         // blocks per row, bytes per row of scales, stages per tile
+    uint32_t tiles_m, tiles_n;
+    __nv_bfloat16* y;
+    uint32_t* flags;
+};
+
+// e2m1 x e2m1 with e8m0 scales -> f32, both operands K-major, M = 128, N = n; the scales of the k-th pair of blocks of a column of scales
+__device__ __forceinline__ uint32_t instr_desc_mxf4(uint32_t n, uint32_t pair)
+{
+    return (2u * pair) << 4 | 1u << 7 | 1u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 | (2u * pair) << 29;
+}
+
+__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scales, uint32_t b_scales, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate) : "memory");
+}
+
+// 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t smem)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc(smem, 0u, 128u)) : "memory");
+}
+
+// 32 consecutive accumulator columns of this thread's lane, as pairs of bf16.
+__device__ __forceinline__ void tmem_ld32_bf16(uint32_t taddr, uint32_t v[16])
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = bf16_pair(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
+}
+
+__device__ __forceinline__ void mm_tile(const MmArgs& a, uint32_t tile, uint32_t& m, uint32_t& n)
+{
+    const uint32_t per_group = kMmGroup * a.tiles_n, group = tile / per_group, in = tile - group * per_group;
+    const uint32_t high = min((uint32_t)kMmGroup, a.tiles_m - group * kMmGroup);
+    n = in / high;
+    m = group * kMmGroup + (in - n * high);
+}
+
+// 16 scales (blocks 16 p .. 16 p + 15) of the rows l, l + 32, l + 64, l + 96 of a group of 128 that starts at row0; zero outside the matrix.
+struct ScaleQuad { uint4 v[4]; };
+__device__ __forceinline__ void load_scales(ScaleQuad& q, const uint8_t* scales, int64_t row0, int64_t rows, uint32_t pitch, uint32_t kb, uint32_t p, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + lane + 32 * i;
+        q.v[i] = row < rows && 16u * p < kb ? __ldg(reinterpret_cast<const uint4*>(scales + row * pitch) + p) : make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+
+// Words j and j + 1 of a quad to the two atoms of a stage; bytes of blocks past the row's last are zero.
+template <int j>
+__device__ __forceinline__ void store_scales(uint32_t smem, const ScaleQuad& q, uint32_t kb, uint32_t first_block, int lane)
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t b = first_block + 4u * (j + h), left = b < kb ? kb - b : 0u, keep = left >= 4u ? 0xffffffffu : (1u << (8u * left)) - 1u;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(smem + h * kScaleAtom + lane * 16), "r"(word_of(q.v[0], j + h) & keep),
+                     "r"(word_of(q.v[1], j + h) & keep), "r"(word_of(q.v[2], j + h) & keep), "r"(word_of(q.v[3], j + h) & keep) : "memory");
+    }
+}
+
+template <int kBn>
+__global__ void __launch_bounds__(kMmThreads, 1)
+mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, MmArgs a)
+{
+    using S = MmShape<kBn>;
+    extern __shared__ uint8_t mm_smem[];
+    const uint32_t base = (smem_u32(mm_smem) + 1023u) & ~1023u;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(mm_smem + (base - smem_u32(mm_smem)) + S::kStages * S::kStage);
+    uint64_t *full = bars, *empty = bars + S::kStages, *acc_full = bars + 2 * S::kStages, *acc_empty = acc_full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) { mbar_init(full + s, 3); mbar_init(empty + s, 1); }      // TMA, scales of W, scales of X
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 8);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, S::kTmem);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_wait();
+
+    const uint32_t tiles = a.tiles_m * a.tiles_n;
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+                uint32_t m, n;
+                mm_tile(a, tile, m, n);
+                for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
+                    const uint32_t s = it % S::kStages, round = it / S::kStages;
+                    if (round > 0) ok = mbar_wait(empty + s, (round - 1u) & 1u);
+                    if (!ok) break;
+                    const uint32_t at = base + s * S::kStage;
+                    mbar_expect(full + s, S::kA + S::kB);
+                    tma_load_2d(at, &w_map, (int)(k * kStageCodes), (int)(m * kMmRows), full + s);
+                    tma_load_2d(at + S::kA, &x_map, (int)(k * kStageCodes), (int)(n * kBn), full + s);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t it = 0, done = 0;
+            for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++done) {
+                if (done > 0) ok = mbar_wait(acc_empty, (done - 1u) & 1u);
+                tc_fence_after();
+                for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
+                    const uint32_t s = it % S::kStages;
+                    ok = mbar_wait_copies(full + s, (it / S::kStages) & 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t at = base + s * S::kStage, sa = at + S::kA + S::kB, sb = sa + 2 * kScaleAtom;
+                    const uint32_t ta = tmem + kBn + (it & 1u) * S::kScaleCols, tb = ta + 8;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        scales_to_tmem(ta + 4 * h, sa + h * kScaleAtom);
+#pragma unroll
+                        for (int g = 0; g < S::kBHalves; ++g) scales_to_tmem(tb + h * 4 * S::kBHalves + 4 * g, sb + (g * 2 + h) * kScaleAtom);
+                    }
+                    const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + S::kA);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)           // 64 columns: 32 bytes on along the rows, two blocks on along the scales
+                        umma_mxf4(tmem, da + 2 * q, db + 2 * q, instr_desc_mxf4(kBn, q & 1), ta + 4 * (q >> 1), tb + 4 * S::kBHalves * (q >> 1), k > 0 || q > 0);
+                    umma_commit(empty + s);
+                }
+                if (ok) umma_commit(acc_full);
+            }
+        }
+    } else if (warp < 4) {
+        const bool of_w = warp == 2;
+        const uint8_t* scales = of_w ? a.w_scales : a.x_scales;
+        const int64_t rows = of_w ? a.n_out : a.tokens;
+        constexpr int kGroups = S::kBHalves;              // W has one group of 128 rows
+        uint32_t it = 0;
+        for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+            uint32_t m, n;
+            mm_tile(a, tile, m, n);
+            const int64_t row0 = of_w ? (int64_t)m * kMmRows : (int64_t)n * kBn;
+            ScaleQuad now[kGroups], next[kGroups];
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+                if (g == 0 || !of_w) load_scales(now[g], scales, row0 + 128 * g, rows, a.pitch, a.kb, 0, lane);
+            for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
+                if ((k & 1u) == 0u) {
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g)
+                        if (g == 0 || !of_w) load_scales(next[g], scales, row0 + 128 * g, rows, a.pitch, a.kb, k / 2 + 1, lane);
+                }
+                const uint32_t s = it % S::kStages, round = it / S::kStages;
+                if (round > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, (round - 1u) & 1u));
+                if (!ok) break;
+                const uint32_t at = base + s * S::kStage + S::kA + S::kB + (of_w ? 0u : 2 * kScaleAtom);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    if (g > 0 && of_w) continue;
+                    if ((k & 1u) == 0u) store_scales<0>(at + 2 * g * kScaleAtom, now[g], a.kb, (k / 2) * 16u, lane);
+                    else {
+                        store_scales<2>(at + 2 * g * kScaleAtom, now[g], a.kb, (k / 2) * 16u, lane);
+                        now[g] = next[g];
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(full + s)) : "memory");
+            }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        constexpr int kCols = kBn / 2;                    // of this warp
+        uint32_t done = 0;
+        for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++done) {
+            uint32_t m, n;
+            mm_tile(a, tile, m, n);
+            ok = __all_sync(0xffffffffu, mbar_wait(acc_full, done & 1u));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t v[kCols / 2];
+#pragma unroll
+            for (int c = 0; c < kCols / 32; ++c) tmem_ld32_bf16(tmem + ((uint32_t)quarter << 21) + half * kCols + 32 * c, v + 16 * c);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(acc_empty)) : "memory");
+            const int64_t row = (int64_t)m * kMmRows + 32 * quarter + lane, token = (int64_t)n * kBn + half * kCols;
+            if (row < a.n_out) {
+                __nv_bfloat16* y = a.y + token * a.n_out + row;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    if (token + c < a.tokens) y[c * a.n_out] = __ushort_as_bfloat16((unsigned short)(v[c >> 1] >> (16 * (c & 1))));
+            }
+        }
+    }
+    if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, S::kTmem);
+}
+
+// The tensor map of a matrix of codes: boxes of 128 bytes by `box` rows, 128-byte swizzle.  (The driver's function asks for a current context: see make_x_map.)
+bool make_code_map(int device, const uint8_t* codes, int64_t pitch, int64_t rows, int box, CUtensorMap* map)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t size[2] = {kStageCodes, (cuuint32_t)box}, steps[2] = {1, 1};
+    auto made = [&] {
+        return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(codes), dims, strides, size, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    return made() || (cudaSetDevice(device) == cudaSuccess && made());
+}
+
+template <int kBn>
+int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* w_codes, int64_t pitch, MmArgs a, cudaStream_t st)
+{
+    CUtensorMap w_map, x_map;
+    if (!make_code_map(ctx->device, w_codes, pitch, a.n_out, kMmRows, &w_map) || !make_code_map(ctx->device, x_codes, pitch, a.tokens, kBn, &x_map)) return LLVQ_ECUDA;
+    if (!set_smem<mx_gemm_kernel<kBn>>(ctx, MmShape<kBn>::kSmem)) return LLVQ_ECUDA;
+    a.tiles_n = (uint32_t)((a.tokens + kBn - 1) / kBn);
+    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles_m * a.tiles_n, (uint64_t)ctx->sm_count);
+    return launch_pdl(mx_gemm_kernel<kBn>, grid, kMmThreads, MmShape<kBn>::kSmem, st, w_map, x_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+}
+
+}  // namespace
+
+extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const uint8_t* d_x_scales, int64_t tokens, const uint8_t* d_codes,
+                            const uint8_t* d_scales, int64_t n_out, int64_t k_in, uint16_t* d_y_bf16, void* stream)
+{
+    if (ctx && ctx->device >= 0 && (n_out == 0 || tokens == 0)) return LLVQ_OK;       // nothing to do: pointers may be null
+    if (!ctx || ctx->device < 0 || n_out < 0 || tokens < 0 || k_in < 0 || !d_y_bf16) return LLVQ_EINVAL;
+    if (k_in > 0 && (!d_x_codes || !d_x_scales || !d_codes || !d_scales)) return LLVQ_EINVAL;
+    if (!aligned(d_x_codes, 16) || !aligned(d_x_scales, 16) || !aligned(d_codes, 16) || !aligned(d_scales, 16) || !aligned(d_y_bf16, 2)) return LLVQ_EALIGN;
+    if (n_out > (1ll << 30) || tokens > (1ll << 30) || k_in > (1ll << 30)) return LLVQ_EUNSUPPORTED;      // TMA coordinates
+    if (((n_out + 127) / 128) * ((tokens + 63) / 64) > (1ll << 31)) return LLVQ_EUNSUPPORTED;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return LLVQ_ECUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (k_in == 0) return cudaMemsetAsync(d_y_bf16, 0, (size_t)n_out * tokens * 2, st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
+    MmArgs a{};
+    a.w_scales = d_scales; a.x_scales = d_x_scales; a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in); a.pitch = (uint32_t)mx_scale_pitch(k_in);
+    a.k_stages = (a.kb + 7) / 8; a.tiles_m = (uint32_t)((n_out + kMmRows - 1) / kMmRows); a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
+    // The widest tile whose rounds over the SMs take least: a stage takes about 128 / 64 / 48 cycles per 64 columns with 256 / 128 / 64 tokens
+    // (the narrowest is held up by its reads of shared memory).
+    auto cost = [&](int bn, int cycles) {
+        const uint64_t t = (uint64_t)a.tiles_m * (uint64_t)((tokens + bn - 1) / bn);
+        return (t + ctx->sm_count - 1) / ctx->sm_count * cycles;
+    };
+    const uint64_t c256 = cost(256, 128), c128 = cost(128, 64), c64 = cost(64, 48);
+    const int64_t pitch = mx_code_pitch(k_in);
+    if (c256 <= c128 && c256 <= c64) return launch_mx_gemm<256>(ctx, d_x_codes, d_codes, pitch, a, st);
+    if (c128 <= c64) return launch_mx_gemm<128>(ctx, d_x_codes, d_codes, pitch, a, st);
+    return launch_mx_gemm<64>(ctx, d_x_codes, d_codes, pitch, a, st);
+}

@@ -52,6 +52,7 @@ def test_host_only_context_refuses_to_launch(P, ctx):
     assert L.llvq_mx_dequant_matrix(ctx._h, vp, vp, 1, 32, vp, 32, None) == 1
     assert L.llvq_mx_gemv(ctx._h, vp, vp, 1, 32, vp, vp, 0, None) == 1
     assert L.llvq_mx_gemm_small_batch(ctx._h, vp, vp, 1, 32, vp, 1, vp, None) == 1
+    assert L.llvq_mx_gemm(ctx._h, vp, vp, 1, vp, vp, 1, 32, vp, None) == 1
     assert L.llvq_embed(ctx._h, vp, 0, 1, 1, vp, 8, 1, 1.0, vp, None) == 1
     assert L.llvq_mx_embed(ctx._h, vp, vp, 1, 1, vp, 8, 1, 1.0, vp, None) == 1
     assert L.llvq_embed_grad(ctx._h, vp, 0, vp, 8, 1, 1, 1, 1.0, -1, 0, vp, 0, vp, None) == 1
@@ -84,6 +85,10 @@ def test_arguments_are_checked_before_the_device(P, ctx):
     with pytest.raises(P.LlvqError) as e:
         P.llvq_mx_gemm_small_batch(ctx, codes, scales, 4, 64, torch.zeros((65, 64), dtype=bf))
     assert e.value.status == 3
+    for tokens, n_out, k_in, y in ((5, 4, 64, None), (4, 5, 64, None), (4, 4, 65, None), (-1, 4, 64, None), (4, 4, -1, None), (4, 4, 64, torch.zeros(15, dtype=bf)),
+                                   (4, 4, 64, torch.zeros(16))):
+        with pytest.raises(AssertionError):
+            P.llvq_mx_gemm(ctx, codes, scales, tokens, codes, scales, n_out, k_in, y)
     with pytest.raises(AssertionError):
         P.llvq_embed(ctx, torch.zeros((4, 8), dtype=torch.float64), torch.zeros(3, dtype=torch.long))
     with pytest.raises(AssertionError):
@@ -108,6 +113,7 @@ def test_host_tensors_are_refused(P, ctx):
               lambda: P.llvq_mx_dequant_matrix(ctx, u8(4, 32), u8(4, 16), 4, 64),
               lambda: P.llvq_mx_gemv(ctx, u8(4, 32), u8(4, 16), 4, 64, torch.zeros(64, dtype=bf)),
               lambda: P.llvq_mx_gemm_small_batch(ctx, u8(4, 32), u8(4, 16), 4, 64, torch.zeros((2, 64), dtype=bf)),
+              lambda: P.llvq_mx_gemm(ctx, u8(4, 32), u8(4, 16), 4, u8(4, 32), u8(4, 16), 4, 64),
               lambda: P.llvq_embed(ctx, torch.zeros((4, 8)), torch.zeros(3, dtype=long)),
               lambda: P.llvq_mx_embed(ctx, u8(4, 32), u8(4, 16), 4, 64, torch.zeros(3, dtype=long)),
               lambda: P.llvq_embed_grad(ctx, torch.zeros((3, 8)), torch.zeros(3, dtype=long), 5)):
