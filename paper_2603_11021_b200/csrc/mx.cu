@@ -2,6 +2,7 @@
 // (see include/llvq.h and mx.cuh).  None of it uses the tables of the context's code: the context gives the device and its error words.
 #include "kernels_common.cuh"
 #include "mx.cuh"
+#include "umma.cuh"
 
 namespace {
 
@@ -104,66 +105,84 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t 
 }
 
 // ---- product with up to 64 rows of activations -------------------------------------------------------------------------------------
-// y[n][r] = sum_k x[n][k] w[r][k] on m16n8k16 tiles: 16 rows of W against 8 of X.  Sums over k may run in any order, so a lane keeps
-// the whole block that its 16-byte load brought: in step s of the eight that 128 columns take, the four places of the tile that belong to
-// the lane (row g = lane / 4, places 2t, 2t+1, 2t+8, 2t+9, t = lane % 4) hold four elements of block t of the 128 columns, and the lane that
-// holds the X side of the same places (column n = lane / 4) reads the same elements.  Elements j and j + 4 of a word of codes sit in the two
-// halves of the word, so a pair of bf16 weights takes two shifts and two logical operations: sign to bit 15, exponent and mantissa to bits
-// 8..6, which is the value times 2^-126, an exact (for 0.5 subnormal) bf16 number; one multiplication by 2^126 times the block's scale makes
-// it the weight, exact wherever the weight is a bf16 number.  Weights are used once, so they never see shared memory.
-// Bound by HBM for few rows of X (4.25 bits per weight, each read once).
-constexpr int kMxChunks = 4;            // chunks of 128 columns whose codes a warp loads together: 16 bytes of scales per row
+// Y[n][r] = sum_k X[n][k] W[r][k] on m16n8k16 tiles in binary16: 16 rows of W against 8 of X.  An e2m1 element is a binary16 number that one
+// instruction per two elements makes; the scale of a block of 32 multiplies the block's sum in binary32.  Activations become binary16 as well:
+// the 512 columns of a chunk of a row of X are multiplied with the power of two that brings their largest finite magnitude to [2^14, 2^15), which
+// leaves every bf16 number exact down to 2^-32 of that magnitude and puts smaller ones off by at most 2^-40 of it, far below the rounding of
+// the sums (binary32, 2^-24 of the same magnitude).
+//
+// A thread block streams W: warp 8 copies the codes of RG x 16 rows and KG x 512 columns per stage with TMA (rows of 128 bytes, swizzled, so that
+// ldmatrix reads 16 bytes of eight rows without conflicts and hands each lane the word of codes whose elements are its own in the tile) and their
+// scales; warps 9 to 12 bring the same columns of X; warps 0 to 7 multiply, 16 rows by 512 columns each, RG x KG = 8.  The stages in flight are
+// what hides the latency of HBM, which bounds the kernel up to about 24 rows of X (4.25 bits per weight, read once); beyond, the products do.
+constexpr int kChunk = 512;                              // columns of a warp's part of a stage
+constexpr int kStreamWarps = 8, kXWarps = 4, kStreamThreads = (kStreamWarps + 1 + kXWarps) * 32;
+constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice
+constexpr uint32_t kStreamCodes = kStreamWarps * 16 * (kChunk / 2), kStreamScales = kStreamWarps * 16 * 16;   // per stage, whatever RG and KG
+constexpr size_t kStreamSmem = 227 * 1024 - 1024;        // dynamic shared memory that a launch may use
 
-__device__ __forceinline__ void mma_bf16(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
-{
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
-// Elements j and j + 4 of a word of codes, as bf16 times 2^-126.
-template <int j>
-__device__ __forceinline__ uint32_t mx_pair(uint32_t w)
-{
-    const uint32_t sign = j == 3 ? w : w << (12 - 4 * j), low = j < 2 ? w << (6 - 4 * j) : w >> (4 * j - 6);
-    return (sign & 0x80008000u) | (low & 0x01c001c0u);
-}
-
-// What a block's pairs are multiplied with, as two bf16: first = 2^126 times the scale where that is a bf16 number (scales up to 2), second = 1;
-// else 2^126 and the scale.
-struct MxFactor { uint32_t first, second; };
-__device__ __forceinline__ MxFactor mx_factor(uint32_t e)
-{
-    const uint32_t f = e <= 128u ? (e + 126u) << 7 : 253u << 7, s = e <= 128u ? 127u << 7 : e == 255u ? 0x7fc0u : e << 7;
-    return {f | f << 16, s | s << 16};
-}
-
-struct MxProduct {
-    const uint8_t *codes, *scales;
-    int64_t n_out, k_in, kb, pitch;
+struct MxStream {
+    int64_t n_out, k_in;
+    uint32_t kb, chunks, tiles;                          // blocks per row, chunks of 512 columns, tiles of 16 RG rows
     const __nv_bfloat16* x;
-    int batch, x_align;                 // elements of X that one load may take: 8, 4, 2 or 1
+    int batch, x_align;                                  // rows of X; elements of X that one load may take: 8, 4, 2 or 1
+    int rg_log2, stages;
+    uint32_t stage_bytes, part_at;                       // of a stage; where the sums of warps that share rows are (KG > 1)
     void* y;
-    int split;                          // warps that share the columns of 16 rows: a power of two
+    uint32_t* flags;
 };
 
+__device__ __forceinline__ void ldsm4(uint32_t r[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ uint32_t lds32(uint32_t addr)
+{
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// The eight elements of a word of codes as binary16 pairs.
+__device__ __forceinline__ void mx_expand_f16(uint32_t w, uint32_t h[4])
+{
+    asm("{\n .reg .b8 b0, b1, b2, b3;\n mov.b32 {b0, b1, b2, b3}, %4;\n"
+        " cvt.rn.f16x2.e2m1x2 %0, b0;\n cvt.rn.f16x2.e2m1x2 %1, b1;\n cvt.rn.f16x2.e2m1x2 %2, b2;\n cvt.rn.f16x2.e2m1x2 %3, b3;\n}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+
+__device__ __forceinline__ void mma_f16(float d[4], const uint32_t a[4], uint32_t b0, uint32_t b1, const float c[4])
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
 // Eight elements of row n of X from column k on; zero past the end.
-__device__ __forceinline__ uint4 load_x8(const MxProduct& a, int n, int64_t k)
+__device__ __forceinline__ uint4 load_x8(const MxStream& a, int n, int64_t k)
 {
     const __nv_bfloat16* p = a.x + (int64_t)n * a.k_in + k;
-    if (k + 8 <= a.k_in && a.x_align == 8) return __ldg(reinterpret_cast<const uint4*>(p));
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (k + 8 <= a.k_in && a.x_align == 4) {
+    const bool whole = k + 8 <= a.k_in;
+    if (whole && a.x_align == 8) return __ldg(reinterpret_cast<const uint4*>(p));
+    if (whole && a.x_align == 4) {
         const uint2 u = __ldg(reinterpret_cast<const uint2*>(p)), v = __ldg(reinterpret_cast<const uint2*>(p) + 1);
         return make_uint4(u.x, u.y, v.x, v.y);
     }
-    if (k + 8 <= a.k_in && a.x_align == 2) {
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (whole && a.x_align == 2) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = __ldg(reinterpret_cast<const uint32_t*>(p) + j);
     } else {
@@ -175,87 +194,227 @@ __device__ __forceinline__ uint4 load_x8(const MxProduct& a, int n, int64_t k)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int kTiles, bool kF32>
-__global__ void __launch_bounds__(kMxThreads)
-mx_product_kernel(MxProduct a)
+// The larger of m and the magnitudes of two bf16, infinities and NaN left out (as bf16 bits).
+__device__ __forceinline__ uint32_t max_finite(uint32_t m, uint32_t pair)
 {
-    __shared__ float part[kMxThreads / 32][kTiles][8][17];     // per warp: 16 rows x 8 columns per tile (17: no two of a column in one bank)
+    const uint32_t lo = pair & 0x7fffu, hi = (pair >> 16) & 0x7fffu;
+    return max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+}
+
+__device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor)
+{
+    return f16_pair(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
+}
+
+// d * 2^h in two steps, for h that binary32 may not hold; NaN for the scale byte 255
+__device__ __forceinline__ float scale_far(float d, uint32_t e, int f)
+{
+    const int h = (int)e - 127 - f, h1 = h / 2, h2 = h - h1;               // |h| <= 127 + 128 + 127 + ...: both halves are normal exponents
+    const float s1 = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(h1 + 127) << 23);
+    return d * s1 * __uint_as_float((uint32_t)(h2 + 127) << 23);
+}
+
+template <int kTiles, bool kF32>
+__global__ void __launch_bounds__(kStreamThreads, 1)
+mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap scales, MxStream a)
+{
+    extern __shared__ uint8_t st_smem[];
+    __shared__ uint64_t full[8], empty[8];
+    const uint32_t base = (smem_u32(st_smem) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rg_n = 1 << a.rg_log2, kg_n = kStreamWarps >> a.rg_log2;
+    const uint32_t rows = 16u << a.rg_log2, steps = (a.chunks + kg_n - 1) / kg_n;      // steps: stages per tile
+    const uint32_t x_at = kStreamCodes + kStreamScales, f_at = x_at + kg_n * a.batch * kXPitch;      // inside a stage
     pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) { mbar_init(full + s, 1 + kXWarps); mbar_init(empty + s, kStreamWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int share = warp % a.split, team = warp / a.split, teams = kMxThreads / 32 / a.split;
-    const int64_t row0 = ((int64_t)blockIdx.x * teams + team) * 16;
-    const int64_t r0 = min(row0 + g, a.n_out - 1), r1 = min(row0 + g + 8, a.n_out - 1);
-    const uint8_t *c0 = a.codes + r0 * a.kb * kMxBlockBytes, *c1 = a.codes + r1 * a.kb * kMxBlockBytes;
-    const uint8_t *s0 = a.scales + r0 * a.pitch, *s1 = a.scales + r1 * a.pitch;
-    float acc[kTiles][4] = {};
-    if (row0 < a.n_out) {
-        for (int64_t b0 = (int64_t)share * (4 * kMxChunks); b0 < a.kb; b0 += (int64_t)a.split * (4 * kMxChunks)) {      // blocks b0 .. b0 + 15
-            uint4 w[2][kMxChunks];
-#pragma unroll
-            for (int c = 0; c < kMxChunks; ++c) {
-                const int64_t b = b0 + 4 * c + t;
-                const bool in = b < a.kb;
-                w[0][c] = in ? __ldcs(reinterpret_cast<const uint4*>(c0 + b * kMxBlockBytes)) : make_uint4(0u, 0u, 0u, 0u);
-                w[1][c] = in ? __ldcs(reinterpret_cast<const uint4*>(c1 + b * kMxBlockBytes)) : make_uint4(0u, 0u, 0u, 0u);
-            }
-            const uint4 e0 = __ldg(reinterpret_cast<const uint4*>(s0 + b0)), e1 = __ldg(reinterpret_cast<const uint4*>(s1 + b0));
-            const uint32_t e[2][4] = {{e0.x, e0.y, e0.z, e0.w}, {e1.x, e1.y, e1.z, e1.w}};
-#pragma unroll
-            for (int c = 0; c < kMxChunks; ++c) {
-                const int64_t b = b0 + 4 * c + t;
-                uint32_t ea = (e[0][c] >> (8 * t)) & 255u, eb = (e[1][c] >> (8 * t)) & 255u;
-                if (b >= a.kb) { ea = 0u; eb = 0u; }            // bytes past the row's last block are not scales
-                const MxFactor fa = mx_factor(ea), fb = mx_factor(eb);
-                const bool large = __any_sync(0xffffffffu, max(ea, eb) > 128u);
-                const uint32_t wa[4] = {w[0][c].x, w[0][c].y, w[0][c].z, w[0][c].w}, wb[4] = {w[1][c].x, w[1][c].y, w[1][c].z, w[1][c].w};
-                uint32_t p[8][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[2 * i][0] = mul_bf16x2(mx_pair<0>(wa[i]), fa.first); p[2 * i][1] = mul_bf16x2(mx_pair<0>(wb[i]), fb.first);
-                    p[2 * i][2] = mul_bf16x2(mx_pair<1>(wa[i]), fa.first); p[2 * i][3] = mul_bf16x2(mx_pair<1>(wb[i]), fb.first);
-                    p[2 * i + 1][0] = mul_bf16x2(mx_pair<2>(wa[i]), fa.first); p[2 * i + 1][1] = mul_bf16x2(mx_pair<2>(wb[i]), fb.first);
-                    p[2 * i + 1][2] = mul_bf16x2(mx_pair<3>(wa[i]), fa.first); p[2 * i + 1][3] = mul_bf16x2(mx_pair<3>(wb[i]), fb.first);
-                }
-                if (large) {
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        p[s][0] = mul_bf16x2(p[s][0], fa.second); p[s][1] = mul_bf16x2(p[s][1], fb.second);
-                        p[s][2] = mul_bf16x2(p[s][2], fa.second); p[s][3] = mul_bf16x2(p[s][3], fb.second);
+    bool ok = true;
+    uint32_t s = 0, phase = 0;                           // stage and its phase
+    auto next = [&] { if (++s == (uint32_t)a.stages) { s = 0; phase ^= 1u; } };
+    if (warp == kStreamWarps) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
+                for (uint32_t step = 0; step < steps; ++step, ++it) {
+                    if (it >= (uint32_t)a.stages) ok = mbar_wait(empty + s, phase ^ 1u);
+                    if (!ok) break;
+                    const uint32_t at = base + s * a.stage_bytes;
+                    mbar_expect(full + s, kStreamCodes + kStreamScales);
+                    for (int g = 0; g < kg_n; ++g) {     // what lies past the end of a row reads as zero
+                        const int chunk = (int)(step * kg_n + g);
+                        tma_load_2d(at + g * rows * (kChunk / 2), &codes, chunk * (kChunk / 2), (int)(tile * rows), full + s);
+                        tma_load_2d(at + g * rows * (kChunk / 2) + rows * 128u, &codes, chunk * (kChunk / 2) + 128, (int)(tile * rows), full + s);
+                        tma_load_2d(at + kStreamCodes + g * rows * 16u, &scales, chunk * 16, (int)(tile * rows), full + s);
                     }
-                }
-#pragma unroll
-                for (int n = 0; n < kTiles; ++n) {
-                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};      // 128 columns by the tensor core, the rest of the sum in binary32 with rounding
-                    const int col = n * 8 + g;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (col < a.batch) v = load_x8(a, col, b * kMxBlock + 8 * i);
-                        mma_bf16(d, p[2 * i], __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
-                        mma_bf16(d, p[2 * i + 1], __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[n][j] += d[j];
+                    next();
                 }
             }
         }
-    }
+    } else if (warp > kStreamWarps) {
+        const int me = warp - kStreamWarps - 1, items = kg_n * a.batch;
+        uint32_t it = 0;
+        for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
+            for (uint32_t step = 0; step < steps; ++step, ++it) {
+                if (it >= (uint32_t)a.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
+                if (!ok) break;
+                const uint32_t at = base + s * a.stage_bytes;
+                constexpr int kAhead = 4;
+                for (int i0 = me; i0 < items; i0 += kXWarps * kAhead) {
+                    uint4 v[kAhead][2];
 #pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
-        part[warp][n][2 * t][g] = acc[n][0]; part[warp][n][2 * t + 1][g] = acc[n][1];
-        part[warp][n][2 * t][g + 8] = acc[n][2]; part[warp][n][2 * t + 1][g + 8] = acc[n][3];
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int i = i0 + u * kXWarps, g = i / a.batch, n = i - g * a.batch;
+                        const int64_t k = (int64_t)(step * kg_n + g) * kChunk + lane * 8;
+                        if (i < items) { v[u][0] = load_x8(a, n, k); v[u][1] = load_x8(a, n, k + 256); }
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int i = i0 + u * kXWarps;
+                        if (i >= items) break;           // the same for the whole warp
+                        uint32_t m = 0;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) m = max_finite(max_finite(max_finite(max_finite(m, v[u][h].x), v[u][h].y), v[u][h].z), v[u][h].w);
+                        m = __reduce_max_sync(0xffffffffu, m);
+                        const int f = min(14 - ((int)(m >> 7) - 127), 127);
+                        const float factor = __uint_as_float((uint32_t)(f + 127) << 23);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            sts128(at + x_at + i * kXPitch + h * 512u + lane * 16u,
+                                   make_uint4(to_f16(v[u][h].x, factor), to_f16(v[u][h].y, factor), to_f16(v[u][h].z, factor), to_f16(v[u][h].w, factor)));
+                        if (lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + f_at + i * 4u), "r"(f) : "memory");
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(full + s)) : "memory");
+                next();
+            }
+        }
+    } else {
+        const int rg = warp & (rg_n - 1), kg = warp >> a.rg_log2, g = lane >> 2, t = lane & 3;
+        // where ldmatrix finds this lane's row: rows 0-7 of a block, 8-15 of it, then the same of the next block
+        const uint32_t mrow = (uint32_t)rg * 16u + (lane & 7) + (lane & 8), mblock = (uint32_t)lane >> 4;
+        const uint32_t row_at = (uint32_t)kg * rows * (kChunk / 2) + mrow * 128u, swizzle = mrow & 7u;
+        const uint32_t scale_at = kStreamCodes + ((uint32_t)kg * rows + rg * 16u + g) * 16u;
+        const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
+            float acc[kTiles][4] = {};
+            for (uint32_t step = 0; step < steps; ++step) {
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
+                if (!ok) break;
+                const uint32_t at = base + s * a.stage_bytes, first = (step * kg_n + kg) * 16u;       // first block
+                if (first < a.kb) {
+                    const uint4 e0 = lds128(at + scale_at), e1 = lds128(at + scale_at + 128u);
+                    uint32_t ea[4] = {e0.x, e0.y, e0.z, e0.w}, eb[4] = {e1.x, e1.y, e1.z, e1.w};
+                    if (a.kb - first < 16u) {            // bytes past the row's last block are not scales: 2^0 instead
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t left = a.kb - first, b = 4u * j, valid = left <= b ? 0u : left - b >= 4u ? 0xffffffffu : (1u << (8u * (left - b))) - 1u;
+                            ea[j] = (ea[j] & valid) | (0x7f7f7f7fu & ~valid);
+                            eb[j] = (eb[j] & valid) | (0x7f7f7f7fu & ~valid);
+                        }
+                    }
+                    // Scales from 2^-63 to 2^64 (bits 7 and 6 differ) and activations whose factor is not far from one: sums times scales stay well inside
+                    // binary32, and the factor is taken off once per chunk.  Else both exponents are added block by block.
+                    uint32_t usual = 0x80808080u;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) usual &= (ea[j] ^ (ea[j] << 1)) & (eb[j] ^ (eb[j] << 1));
+                    int f[kTiles][2];
+                    bool near = usual == 0x80808080u;
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            f[n][c] = (int)lds32(at + f_at + (kg * a.batch + min(n * 8 + 2 * t + c, a.batch - 1)) * 4u);
+                            near &= f[n][c] >= -30 && f[n][c] <= 50;
+                        }
+                    const bool fast = __all_sync(0xffffffffu, near);
+                    float part[kTiles][4] = {};
+#pragma unroll 2
+                    for (int b = 0; b < 16; b += 2) {
+                        uint32_t w[4], h[4][4];
+                        ldsm4(w, at + row_at + (b >> 3) * rows * 128u + ((((uint32_t)b & 7u) + mblock) ^ swizzle) * 16u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mx_expand_f16(w[i], h[i]);
+                        const uint32_t wa = b < 4 ? ea[0] : b < 8 ? ea[1] : b < 12 ? ea[2] : ea[3], wb = b < 4 ? eb[0] : b < 8 ? eb[1] : b < 12 ? eb[2] : eb[3];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const uint32_t byte_a = (wa >> (8 * ((b + q) & 3))) & 255u, byte_b = (wb >> (8 * ((b + q) & 3))) & 255u;
+                            const float sa = __uint_as_float(byte_a << 23), sb = __uint_as_float(byte_b << 23);
+                            const uint32_t lo[4] = {h[2 * q][0], h[2 * q + 1][0], h[2 * q][1], h[2 * q + 1][1]};
+                            const uint32_t hi[4] = {h[2 * q][2], h[2 * q + 1][2], h[2 * q][3], h[2 * q + 1][3]};
+#pragma unroll
+                            for (int n = 0; n < kTiles; ++n) {
+                                const uint4 x = lds128(at + x_at + (kg * a.batch + min(n * 8 + g, a.batch - 1)) * kXPitch + (b + q) * 64u + t * 16u);
+                                float d[4];
+                                mma_f16(d, lo, x.x, x.y, zero);
+                                mma_f16(d, hi, x.z, x.w, d);
+                                if (fast) {
+                                    part[n][0] += d[0] * sa; part[n][1] += d[1] * sa;
+                                    part[n][2] += d[2] * sb; part[n][3] += d[3] * sb;
+                                } else {
+                                    part[n][0] += scale_far(d[0], byte_a, f[n][0]); part[n][1] += scale_far(d[1], byte_a, f[n][1]);
+                                    part[n][2] += scale_far(d[2], byte_b, f[n][0]); part[n][3] += scale_far(d[3], byte_b, f[n][1]);
+                                }
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[n][j] += fast ? part[n][j] * __uint_as_float((uint32_t)(127 - f[n][j & 1]) << 23) : part[n][j];
+                }
+                __syncwarp();
+                if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(empty + s)) : "memory");
+                next();
+            }
+            if (!ok) break;
+            const int64_t row0 = (int64_t)tile * rows;
+            auto put = [&](int n, int64_t row, float v) {
+                if (n >= a.batch || row >= a.n_out) return;
+                if (kF32) static_cast<float*>(a.y)[(int64_t)n * a.n_out + row] = v;
+                else static_cast<__nv_bfloat16*>(a.y)[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(v);
+            };
+            if (kg_n == 1) {
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) put(n * 8 + 2 * t + (j & 1), row0 + rg * 16 + g + 8 * (j >> 1), acc[n][j]);
+            } else {
+                float* part = reinterpret_cast<float*>(st_smem + (base - smem_u32(st_smem)) + a.part_at);       // [kg][column][row]
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) part[(kg * kTiles * 8 + n * 8 + 2 * t + (j & 1)) * (int)rows + rg * 16 + g + 8 * (j >> 1)] = acc[n][j];
+                asm volatile("bar.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");
+                for (int i = threadIdx.x; i < a.batch * (int)rows; i += kStreamWarps * 32) {
+                    const int n = i / (int)rows, r = i & (int)(rows - 1);
+                    float v = 0.0f;
+                    for (int k = 0; k < kg_n; ++k) v += part[(k * kTiles * 8 + n) * (int)rows + r];
+                    put(n, row0 + r, v);
+                }
+                asm volatile("bar.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");      // the sums are read before the next tile's are written
+            }
+        }
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < teams * 16 * a.batch; i += kMxThreads) {
-        const int r = i & 15, m = (i >> 4) % teams, n = (i >> 4) / teams;
-        const int64_t row = ((int64_t)blockIdx.x * teams + m) * 16 + r;
-        if (row >= a.n_out) continue;
-        float s = 0.0f;
-        for (int j = 0; j < a.split; ++j) s += part[m * a.split + j][n >> 3][n & 7][r];
-        if (kF32) static_cast<float*>(a.y)[(int64_t)n * a.n_out + row] = s;
-        else static_cast<__nv_bfloat16*>(a.y)[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(s);
-    }
+    if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
+}
+
+// A tensor map of rows of bytes: boxes of `width` bytes by `box` rows.  (The driver's function asks for a current context: see make_x_map.)
+bool make_byte_map(int device, const uint8_t* p, int64_t pitch, int64_t rows, int width, int box, bool swizzle, CUtensorMap* map)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t size[2] = {(cuuint32_t)width, (cuuint32_t)box}, steps[2] = {1, 1};
+    auto made = [&] {
+        return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, size, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    return made() || (cudaSetDevice(device) == cudaSuccess && made());
 }
 
 // Sizes whose byte counts leave 63 bits, or dimensions that the kernels' indices do not hold.
@@ -278,31 +437,61 @@ cudaError_t launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t l
     return launch_pdl(mx_quantize_kernel<T>, (unsigned)ctas, kMxThreads, 0, st, static_cast<const T*>(x), rows, cols, ld, pieces, wide, codes, scales);
 }
 
+template <int kTiles>
+int launch_stream(const llvq_ctx* ctx, const CUtensorMap& codes, const CUtensorMap& scales, const MxStream& a, unsigned grid, size_t smem, int y_dtype, cudaStream_t st)
+{
+    cudaError_t r;
+    if (y_dtype == LLVQ_F32) {
+        if (!set_smem<mx_stream_kernel<kTiles, true>>(ctx, smem)) return LLVQ_ECUDA;
+        r = launch_pdl(mx_stream_kernel<kTiles, true>, grid, kStreamThreads, smem, st, codes, scales, a);
+    } else {
+        if (!set_smem<mx_stream_kernel<kTiles, false>>(ctx, smem)) return LLVQ_ECUDA;
+        r = launch_pdl(mx_stream_kernel<kTiles, false>, grid, kStreamThreads, smem, st, codes, scales, a);
+    }
+    return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+}
+
 int mx_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x, int batch, void* d_y,
                int y_dtype, cudaStream_t st)
 {
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return LLVQ_ECUDA;
     if (k_in == 0) return cudaMemsetAsync(d_y, 0, (size_t)n_out * batch * (y_dtype == LLVQ_F32 ? 4 : 2), st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
-    MxProduct a{};
-    a.codes = d_codes; a.scales = d_scales; a.n_out = n_out; a.k_in = k_in; a.kb = mx_blocks(k_in); a.pitch = mx_scale_pitch(k_in);
-    a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y;
+    MxStream a{};
+    a.n_out = n_out; a.k_in = k_in; a.kb = (uint32_t)mx_blocks(k_in); a.chunks = (a.kb + 15) / 16;
+    a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y; a.flags = ctx->dev.flags;
     a.x_align = 8;
     while (a.x_align > 1 && (!aligned(d_x, 2 * (size_t)a.x_align) || (batch > 1 && k_in % a.x_align != 0))) a.x_align /= 2;
-    a.split = 1;
-    while (a.split < kMxThreads / 32 && a.split * 4 * kMxChunks < a.kb) a.split *= 2;
-    const int64_t rows_per_cta = 16 * (kMxThreads / 32 / a.split), ctas = (n_out + rows_per_cta - 1) / rows_per_cta;
-    const int tiles = (batch + 7) / 8;
-    cudaError_t r;
-#define MX_PRODUCT(TILES)                                                                                                                     \
-    r = y_dtype == LLVQ_F32 ? launch_pdl(mx_product_kernel<TILES, true>, (unsigned)ctas, kMxThreads, 0, st, a)                                \
-                            : launch_pdl(mx_product_kernel<TILES, false>, (unsigned)ctas, kMxThreads, 0, st, a)
-    if (tiles <= 1) MX_PRODUCT(1);
-    else if (tiles <= 2) MX_PRODUCT(2);
-    else if (tiles <= 4) MX_PRODUCT(4);
-    else MX_PRODUCT(8);
-#undef MX_PRODUCT
-    return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    // Rows of a tile: what takes the fewest rounds over the SMs, counted in rows, with a quarter of the smallest tile on top for the end of a tile
+    // and no more warps along a row than it has chunks.
+    uint64_t best = ~0ull;
+    for (int l = 3; l >= 0; --l) {
+        if (l < 3 && (8u >> (l + 1)) >= a.chunks) break;
+        const uint64_t tiles = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), cost = (tiles + ctx->sm_count - 1) / ctx->sm_count * ((4u << l) + 1u);
+        if (cost < best) { best = cost; a.rg_log2 = l; a.tiles = (uint32_t)tiles; }
+    }
+    const int kg = kStreamWarps >> a.rg_log2, tiles = (batch + 7) / 8, kept = tiles <= 4 ? tiles : 8;
+    a.stage_bytes = (kStreamCodes + kStreamScales + (uint32_t)(kg * batch) * (kXPitch + 4u) + 1023u) & ~1023u;
+    const uint32_t part = kg > 1 ? (uint32_t)kg * kept * 8u * (16u << a.rg_log2) * 4u : 0u;
+    a.stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / a.stage_bytes);
+    if (a.stages < 2) {                                  // wide batches: whole rows per warp
+        a.rg_log2 = 3; a.tiles = (uint32_t)((n_out + 127) / 128);
+        a.stage_bytes = (kStreamCodes + kStreamScales + (uint32_t)batch * (kXPitch + 4u) + 1023u) & ~1023u;
+        a.stages = (int)std::min<size_t>(6, (kStreamSmem - 1024) / a.stage_bytes);
+    }
+    a.part_at = (uint32_t)a.stages * a.stage_bytes;
+    const size_t smem = 1024 + a.part_at + (a.rg_log2 < 3 ? part : 0u);
+    CUtensorMap codes, scales;
+    if (!make_byte_map(ctx->device, d_codes, mx_code_pitch(k_in), n_out, 128, 16 << a.rg_log2, true, &codes) ||
+        !make_byte_map(ctx->device, d_scales, mx_scale_pitch(k_in), n_out, 16, 16 << a.rg_log2, false, &scales)) return LLVQ_ECUDA;
+    const unsigned grid = std::min<unsigned>(a.tiles, (unsigned)ctx->sm_count);
+    switch (kept) {
+        case 1: return launch_stream<1>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 2: return launch_stream<2>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 3: return launch_stream<3>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 4: return launch_stream<4>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        default: return launch_stream<8>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+    }
 }
 
 }  // namespace
@@ -337,7 +526,7 @@ int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_s
     if (int e = mx_check(ctx, k_in == 0, d_codes, d_scales)) return e;
     if ((!d_x_bf16 && k_in != 0) || !d_y || n_out < 0 || k_in < 0 || (y_dtype != LLVQ_F32 && y_dtype != LLVQ_BF16)) return LLVQ_EINVAL;
     if (!aligned(d_x_bf16, 2) || !aligned(d_y, y_dtype == LLVQ_F32 ? 4 : 2)) return LLVQ_EALIGN;
-    if (mx_too_large(n_out, k_in)) return LLVQ_EUNSUPPORTED;
+    if (n_out > (1ll << 30) || k_in > (1ll << 30)) return LLVQ_EUNSUPPORTED;      // TMA coordinates
     return mx_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, 1, d_y, y_dtype, (cudaStream_t)stream);
 }
 
@@ -348,7 +537,7 @@ int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const 
     if (int e = mx_check(ctx, k_in == 0, d_codes, d_scales)) return e;
     if ((!d_x_bf16 && k_in != 0) || !d_y_bf16 || n_out < 0 || k_in < 0 || batch < 0) return LLVQ_EINVAL;
     if (!aligned(d_x_bf16, 2) || !aligned(d_y_bf16, 2)) return LLVQ_EALIGN;
-    if (batch > 64 || mx_too_large(n_out, k_in)) return LLVQ_EUNSUPPORTED;
+    if (batch > 64 || n_out > (1ll << 30) || k_in > (1ll << 30)) return LLVQ_EUNSUPPORTED;
     return mx_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, LLVQ_BF16, (cudaStream_t)stream);
 }
 
