@@ -1,5 +1,7 @@
 // Quantisation to microscaled 4-bit floating point, back to bf16, and products of such a matrix with up to 64 rows of bf16 activations
 // (see include/llvq.h and mx.cuh).  None of it uses the tables of the context's code: the context gives the device and its error words.
+#include <type_traits>
+
 #include "kernels_common.cuh"
 #include "mx.cuh"
 #include "umma.cuh"
@@ -113,12 +115,15 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t 
 //
 // A thread block streams W: warp 8 copies the codes of RG x 16 rows and KG x 512 columns per stage with TMA (rows of 128 bytes, swizzled, so that
 // ldmatrix reads 16 bytes of eight rows without conflicts and hands each lane the word of codes whose elements are its own in the tile) and their
-// scales; warps 9 to 12 bring the same columns of X; warps 0 to 7 multiply, 16 rows by 512 columns each, RG x KG = 8.  The stages in flight are
+// scales; warps 9 to 12 bring the same columns of X; warps 0 to 7 multiply, 16 rows by 512 columns each, RG x KG = 8 (up to 16 rows of X: 16 warps).  The stages in flight are
 // what hides the latency of HBM, which bounds the kernel up to about 24 rows of X (4.25 bits per weight, read once); beyond, the products do.
 constexpr int kChunk = 512;                              // columns of a warp's part of a stage
-constexpr int kStreamWarps = 8, kXWarps = 4, kStreamThreads = (kStreamWarps + 1 + kXWarps) * 32;
+constexpr int kXWarps = 4;
 constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice
-constexpr uint32_t kStreamCodes = kStreamWarps * 16 * (kChunk / 2), kStreamScales = kStreamWarps * 16 * 16;   // per stage, whatever RG and KG
+template <int kWarps> struct Stream {                    // kWarps multiply
+    static constexpr int kThreads = (kWarps + 1 + kXWarps) * 32;
+    static constexpr uint32_t kCodes = kWarps * 16 * (kChunk / 2), kScales = kWarps * 16 * 16;      // bytes per stage, whatever RG and KG
+};
 constexpr size_t kStreamSmem = 227 * 1024 - 1024;        // dynamic shared memory that a launch may use
 
 struct MxStream {
@@ -214,20 +219,21 @@ __device__ __forceinline__ float scale_far(float d, uint32_t e, int f)
     return d * s1 * __uint_as_float((uint32_t)(h2 + 127) << 23);
 }
 
-template <int kTiles, bool kF32>
-__global__ void __launch_bounds__(kStreamThreads, 1)
+template <int kWarps, int kTiles, bool kF32>
+__global__ void __launch_bounds__(Stream<kWarps>::kThreads, 1)
 mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap scales, MxStream a)
 {
+    constexpr uint32_t kCodes = Stream<kWarps>::kCodes, kScales = Stream<kWarps>::kScales;
     extern __shared__ uint8_t st_smem[];
     __shared__ uint64_t full[8], empty[8];
     const uint32_t base = (smem_u32(st_smem) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rg_n = 1 << a.rg_log2, kg_n = kStreamWarps >> a.rg_log2;
+    const int rg_n = 1 << a.rg_log2, kg_n = kWarps >> a.rg_log2;
     const uint32_t rows = 16u << a.rg_log2, steps = (a.chunks + kg_n - 1) / kg_n;      // steps: stages per tile
-    const uint32_t x_at = kStreamCodes + kStreamScales, f_at = x_at + kg_n * a.batch * kXPitch;      // inside a stage
+    const uint32_t x_at = kCodes + kScales, f_at = x_at + kg_n * a.batch * kXPitch;      // inside a stage
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < a.stages; ++s) { mbar_init(full + s, 1 + kXWarps); mbar_init(empty + s, kStreamWarps); }
+        for (int s = 0; s < a.stages; ++s) { mbar_init(full + s, 1 + kXWarps); mbar_init(empty + s, kWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -235,7 +241,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
     bool ok = true;
     uint32_t s = 0, phase = 0;                           // stage and its phase
     auto next = [&] { if (++s == (uint32_t)a.stages) { s = 0; phase ^= 1u; } };
-    if (warp == kStreamWarps) {
+    if (warp == kWarps) {
         if (lane == 0) {
             uint32_t it = 0;
             for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
@@ -243,19 +249,19 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                     if (it >= (uint32_t)a.stages) ok = mbar_wait(empty + s, phase ^ 1u);
                     if (!ok) break;
                     const uint32_t at = base + s * a.stage_bytes;
-                    mbar_expect(full + s, kStreamCodes + kStreamScales);
+                    mbar_expect(full + s, kCodes + kScales);
                     for (int g = 0; g < kg_n; ++g) {     // what lies past the end of a row reads as zero
                         const int chunk = (int)(step * kg_n + g);
                         tma_load_2d(at + g * rows * (kChunk / 2), &codes, chunk * (kChunk / 2), (int)(tile * rows), full + s);
                         tma_load_2d(at + g * rows * (kChunk / 2) + rows * 128u, &codes, chunk * (kChunk / 2) + 128, (int)(tile * rows), full + s);
-                        tma_load_2d(at + kStreamCodes + g * rows * 16u, &scales, chunk * 16, (int)(tile * rows), full + s);
+                        tma_load_2d(at + kCodes + g * rows * 16u, &scales, chunk * 16, (int)(tile * rows), full + s);
                     }
                     next();
                 }
             }
         }
-    } else if (warp > kStreamWarps) {
-        const int me = warp - kStreamWarps - 1, items = kg_n * a.batch;
+    } else if (warp > kWarps) {
+        const int me = warp - kWarps - 1, items = kg_n * a.batch;
         uint32_t it = 0;
         for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
             for (uint32_t step = 0; step < steps; ++step, ++it) {
@@ -298,7 +304,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
         // where ldmatrix finds this lane's row: rows 0-7 of a block, 8-15 of it, then the same of the next block
         const uint32_t mrow = (uint32_t)rg * 16u + (lane & 7) + (lane & 8), mblock = (uint32_t)lane >> 4;
         const uint32_t row_at = (uint32_t)kg * rows * (kChunk / 2) + mrow * 128u, swizzle = mrow & 7u;
-        const uint32_t scale_at = kStreamCodes + ((uint32_t)kg * rows + rg * 16u + g) * 16u;
+        const uint32_t scale_at = kCodes + ((uint32_t)kg * rows + rg * 16u + g) * 16u;
         const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
             float acc[kTiles][4] = {};
@@ -331,41 +337,59 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                             f[n][c] = (int)lds32(at + f_at + (kg * a.batch + min(n * 8 + 2 * t + c, a.batch - 1)) * 4u);
                             near &= f[n][c] >= -30 && f[n][c] <= 50;
                         }
-                    const bool fast = __all_sync(0xffffffffu, near);
+                    const uint32_t codes_at = (at + row_at) | ((mblock ^ swizzle) << 4), x_row = at + x_at + kg * a.batch * kXPitch + t * 16u;
+                    uint32_t xs[kTiles];                 // this lane's row of X for each tile: the last one again where there are no more
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n) xs[n] = x_row + min(n * 8 + g, a.batch - 1) * kXPitch;
                     float part[kTiles][4] = {};
-#pragma unroll 2
-                    for (int b = 0; b < 16; b += 2) {
-                        uint32_t w[4], h[4][4];
-                        ldsm4(w, at + row_at + (b >> 3) * rows * 128u + ((((uint32_t)b & 7u) + mblock) ^ swizzle) * 16u);
+                    auto chunk = [&](auto fast) {
+#pragma unroll (kTiles <= 2 ? 2 : 1)
+                        for (int box = 0; box < 2; ++box) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mx_expand_f16(w[i], h[i]);
-                        const uint32_t wa = b < 4 ? ea[0] : b < 8 ? ea[1] : b < 12 ? ea[2] : ea[3], wb = b < 4 ? eb[0] : b < 8 ? eb[1] : b < 12 ? eb[2] : eb[3];
+                            for (int b = 0; b < 8; b += 2) {
+                                uint32_t w[4], h[4][4];
+                                ldsm4(w, (codes_at + box * rows * 128u) ^ (b * 16u));
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const uint32_t byte_a = (wa >> (8 * ((b + q) & 3))) & 255u, byte_b = (wb >> (8 * ((b + q) & 3))) & 255u;
-                            const float sa = __uint_as_float(byte_a << 23), sb = __uint_as_float(byte_b << 23);
-                            const uint32_t lo[4] = {h[2 * q][0], h[2 * q + 1][0], h[2 * q][1], h[2 * q + 1][1]};
-                            const uint32_t hi[4] = {h[2 * q][2], h[2 * q + 1][2], h[2 * q][3], h[2 * q + 1][3]};
+                                for (int i = 0; i < 4; ++i) mx_expand_f16(w[i], h[i]);
+                                const uint32_t wa = box == 0 ? ea[b >> 2] : ea[2 + (b >> 2)], wb = box == 0 ? eb[b >> 2] : eb[2 + (b >> 2)];
 #pragma unroll
-                            for (int n = 0; n < kTiles; ++n) {
-                                const uint4 x = lds128(at + x_at + (kg * a.batch + min(n * 8 + g, a.batch - 1)) * kXPitch + (b + q) * 64u + t * 16u);
-                                float d[4];
-                                mma_f16(d, lo, x.x, x.y, zero);
-                                mma_f16(d, hi, x.z, x.w, d);
-                                if (fast) {
-                                    part[n][0] += d[0] * sa; part[n][1] += d[1] * sa;
-                                    part[n][2] += d[2] * sb; part[n][3] += d[3] * sb;
-                                } else {
-                                    part[n][0] += scale_far(d[0], byte_a, f[n][0]); part[n][1] += scale_far(d[1], byte_a, f[n][1]);
-                                    part[n][2] += scale_far(d[2], byte_b, f[n][0]); part[n][3] += scale_far(d[3], byte_b, f[n][1]);
+                                for (int q = 0; q < 2; ++q) {
+                                    constexpr uint32_t kExponent = 0x7f800000u;
+                                    const int j = (b + q) & 3;
+                                    const uint32_t sa = (j < 3 ? wa << (23 - 8 * j) : wa >> 1) & kExponent, sb = (j < 3 ? wb << (23 - 8 * j) : wb >> 1) & kExponent;
+                                    const uint32_t lo[4] = {h[2 * q][0], h[2 * q + 1][0], h[2 * q][1], h[2 * q + 1][1]};
+                                    const uint32_t hi[4] = {h[2 * q][2], h[2 * q + 1][2], h[2 * q][3], h[2 * q + 1][3]};
+#pragma unroll
+                                    for (int n = 0; n < kTiles; ++n) {
+                                        const uint4 x = lds128(xs[n] + box * 512u + (b + q) * 64u);
+                                        float d[4];
+                                        mma_f16(d, lo, x.x, x.y, zero);
+                                        mma_f16(d, hi, x.z, x.w, d);
+                                        if constexpr (decltype(fast)::value) {
+                                            part[n][0] += d[0] * __uint_as_float(sa); part[n][1] += d[1] * __uint_as_float(sa);
+                                            part[n][2] += d[2] * __uint_as_float(sb); part[n][3] += d[3] * __uint_as_float(sb);
+                                        } else {
+                                            part[n][0] += scale_far(d[0], sa >> 23, f[n][0]); part[n][1] += scale_far(d[1], sa >> 23, f[n][1]);
+                                            part[n][2] += scale_far(d[2], sb >> 23, f[n][0]); part[n][3] += scale_far(d[3], sb >> 23, f[n][1]);
+                                        }
+                                    }
                                 }
                             }
                         }
+                    };
+                    if (__all_sync(0xffffffffu, near)) {
+                        chunk(std::true_type{});
+#pragma unroll
+                        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[n][j] += part[n][j] * __uint_as_float((uint32_t)(127 - f[n][j & 1]) << 23);
+                    } else {
+                        chunk(std::false_type{});
+#pragma unroll
+                        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) acc[n][j] += part[n][j];
                     }
-#pragma unroll
-                    for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[n][j] += fast ? part[n][j] * __uint_as_float((uint32_t)(127 - f[n][j & 1]) << 23) : part[n][j];
                 }
                 __syncwarp();
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(empty + s)) : "memory");
@@ -389,14 +413,14 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                 for (int n = 0; n < kTiles; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) part[(kg * kTiles * 8 + n * 8 + 2 * t + (j & 1)) * (int)rows + rg * 16 + g + 8 * (j >> 1)] = acc[n][j];
-                asm volatile("bar.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");
-                for (int i = threadIdx.x; i < a.batch * (int)rows; i += kStreamWarps * 32) {
+                asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+                for (int i = threadIdx.x; i < a.batch * (int)rows; i += kWarps * 32) {
                     const int n = i / (int)rows, r = i & (int)(rows - 1);
                     float v = 0.0f;
                     for (int k = 0; k < kg_n; ++k) v += part[(k * kTiles * 8 + n) * (int)rows + r];
                     put(n, row0 + r, v);
                 }
-                asm volatile("bar.sync 1, %0;" ::"n"(kStreamWarps * 32) : "memory");      // the sums are read before the next tile's are written
+                asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");      // the sums are read before the next tile's are written
             }
         }
     }
@@ -437,16 +461,16 @@ cudaError_t launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t l
     return launch_pdl(mx_quantize_kernel<T>, (unsigned)ctas, kMxThreads, 0, st, static_cast<const T*>(x), rows, cols, ld, pieces, wide, codes, scales);
 }
 
-template <int kTiles>
+template <int kWarps, int kTiles>
 int launch_stream(const llvq_ctx* ctx, const CUtensorMap& codes, const CUtensorMap& scales, const MxStream& a, unsigned grid, size_t smem, int y_dtype, cudaStream_t st)
 {
     cudaError_t r;
     if (y_dtype == LLVQ_F32) {
-        if (!set_smem<mx_stream_kernel<kTiles, true>>(ctx, smem)) return LLVQ_ECUDA;
-        r = launch_pdl(mx_stream_kernel<kTiles, true>, grid, kStreamThreads, smem, st, codes, scales, a);
+        if (!set_smem<mx_stream_kernel<kWarps, kTiles, true>>(ctx, smem)) return LLVQ_ECUDA;
+        r = launch_pdl(mx_stream_kernel<kWarps, kTiles, true>, grid, Stream<kWarps>::kThreads, smem, st, codes, scales, a);
     } else {
-        if (!set_smem<mx_stream_kernel<kTiles, false>>(ctx, smem)) return LLVQ_ECUDA;
-        r = launch_pdl(mx_stream_kernel<kTiles, false>, grid, kStreamThreads, smem, st, codes, scales, a);
+        if (!set_smem<mx_stream_kernel<kWarps, kTiles, false>>(ctx, smem)) return LLVQ_ECUDA;
+        r = launch_pdl(mx_stream_kernel<kWarps, kTiles, false>, grid, Stream<kWarps>::kThreads, smem, st, codes, scales, a);
     }
     return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
@@ -462,35 +486,36 @@ int mx_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_sca
     a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y; a.flags = ctx->dev.flags;
     a.x_align = 8;
     while (a.x_align > 1 && (!aligned(d_x, 2 * (size_t)a.x_align) || (batch > 1 && k_in % a.x_align != 0))) a.x_align /= 2;
-    // Rows of a tile: what takes the fewest rounds over the SMs, counted in rows, with a quarter of the smallest tile on top for the end of a tile
-    // and no more warps along a row than it has chunks.
+    const int tiles = (batch + 7) / 8, kept = tiles <= 4 ? tiles : 8, warps = tiles <= 2 ? 16 : 8, most = warps == 16 ? 4 : 3;
+    const uint32_t fixed = warps == 16 ? Stream<16>::kCodes + Stream<16>::kScales : Stream<8>::kCodes + Stream<8>::kScales;
+    // Rows of a tile: what takes the fewest rounds over the SMs, counted in rows, with a quarter of the smallest tile on top for the end of a tile,
+    // no more warps along a row than it has chunks, and two stages at least.
     uint64_t best = ~0ull;
-    for (int l = 3; l >= 0; --l) {
-        if (l < 3 && (8u >> (l + 1)) >= a.chunks) break;
-        const uint64_t tiles = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), cost = (tiles + ctx->sm_count - 1) / ctx->sm_count * ((4u << l) + 1u);
-        if (cost < best) { best = cost; a.rg_log2 = l; a.tiles = (uint32_t)tiles; }
+    size_t smem = 0;
+    for (int l = most; l >= 0; --l) {
+        const int kg = warps >> l;
+        if (l < most && kg / 2 >= (int)a.chunks) break;
+        const uint32_t stage = (fixed + (uint32_t)(kg * batch) * (kXPitch + 4u) + 1023u) & ~1023u;
+        const uint32_t part = kg > 1 ? (uint32_t)kg * kept * 8u * (16u << l) * 4u : 0u;
+        const int stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / stage);
+        if (stages < 2) continue;
+        const uint64_t count = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), cost = (count + ctx->sm_count - 1) / ctx->sm_count * ((4u << l) + 1u);
+        if (cost >= best) continue;
+        best = cost;
+        a.rg_log2 = l; a.tiles = (uint32_t)count; a.stage_bytes = stage; a.stages = stages; a.part_at = (uint32_t)stages * stage;
+        smem = 1024 + a.part_at + part;
     }
-    const int kg = kStreamWarps >> a.rg_log2, tiles = (batch + 7) / 8, kept = tiles <= 4 ? tiles : 8;
-    a.stage_bytes = (kStreamCodes + kStreamScales + (uint32_t)(kg * batch) * (kXPitch + 4u) + 1023u) & ~1023u;
-    const uint32_t part = kg > 1 ? (uint32_t)kg * kept * 8u * (16u << a.rg_log2) * 4u : 0u;
-    a.stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / a.stage_bytes);
-    if (a.stages < 2) {                                  // wide batches: whole rows per warp
-        a.rg_log2 = 3; a.tiles = (uint32_t)((n_out + 127) / 128);
-        a.stage_bytes = (kStreamCodes + kStreamScales + (uint32_t)batch * (kXPitch + 4u) + 1023u) & ~1023u;
-        a.stages = (int)std::min<size_t>(6, (kStreamSmem - 1024) / a.stage_bytes);
-    }
-    a.part_at = (uint32_t)a.stages * a.stage_bytes;
-    const size_t smem = 1024 + a.part_at + (a.rg_log2 < 3 ? part : 0u);
+    if (best == ~0ull) return LLVQ_EUNSUPPORTED;
     CUtensorMap codes, scales;
     if (!make_byte_map(ctx->device, d_codes, mx_code_pitch(k_in), n_out, 128, 16 << a.rg_log2, true, &codes) ||
         !make_byte_map(ctx->device, d_scales, mx_scale_pitch(k_in), n_out, 16, 16 << a.rg_log2, false, &scales)) return LLVQ_ECUDA;
     const unsigned grid = std::min<unsigned>(a.tiles, (unsigned)ctx->sm_count);
     switch (kept) {
-        case 1: return launch_stream<1>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 2: return launch_stream<2>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 3: return launch_stream<3>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 4: return launch_stream<4>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        default: return launch_stream<8>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 1: return launch_stream<16, 1>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 2: return launch_stream<16, 2>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 3: return launch_stream<8, 3>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        case 4: return launch_stream<8, 4>(ctx, codes, scales, a, grid, smem, y_dtype, st);
+        default: return launch_stream<8, 8>(ctx, codes, scales, a, grid, smem, y_dtype, st);
     }
 }
 
