@@ -432,15 +432,19 @@ int llvq_mx_dequant_matrix(const llvq_ctx* ctx, const uint8_t* d_codes, const ui
                            uint16_t* d_w_bf16, int64_t ld, void* stream);
 
 /*
- * y = W x and Y[b][i] = sum_k X[b][k] W[i][k] (batch <= 64) with W (n_out x k_in) in 4 bits and bf16 activations; the weights are the
- * bf16 values of llvq_mx_dequant_matrix, products are accumulated in binary32, in an order that the sizes alone fix.
+ * y = W x and Y[b][i] = sum_k X[b][k] W[i][k] (batch <= 64) with W (n_out x k_in) in 4 bits and bf16 activations; products are
+ * accumulated in binary32, in an order that the sizes alone fix.  The activations enter as binary16 or e4m3 numbers with powers of two
+ * beside them: exact down to 2^-19 of the largest finite one of their 32 columns, off by at most 2^-27 of that one below.
  * d_x_bf16: [batch][k_in], 2-byte aligned, any k_in (rows on 16-byte boundaries are read fastest).  d_y: [n_out] float or bf16
- * bits; d_y_bf16: [batch][n_out] bf16 bits.
+ * bits; d_y_bf16: [batch][n_out] bf16 bits.  Sizes up to 2^30.  d_work: 256-byte aligned device memory of llvq_mx_small_batch_bytes
+ * bytes (0, and then not used, for batch 1, where there is nothing to do, and for sizes that are not supported), which belongs to the
+ * call until it is done: calls that may overlap need one each.
  */
 int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in,
                  const uint16_t* d_x_bf16, void* d_y, int y_dtype, void* stream);
+size_t llvq_mx_small_batch_bytes(const llvq_ctx* ctx, int64_t n_out, int64_t k_in, int batch);
 int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in,
-                             const uint16_t* d_x_bf16, int batch, uint16_t* d_y_bf16, void* stream);
+                             const uint16_t* d_x_bf16, int batch, uint16_t* d_y_bf16, void* d_work, void* stream);
 
 /*
  * Y[t][i] = sum_k X[t][k] W[i][k] with both operands in 4 bits (a prompt's activations by llvq_mx_quantize, any number of tokens) on the

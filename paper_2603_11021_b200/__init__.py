@@ -56,7 +56,7 @@ EXPORTS = [
     "llvq_gemm_small_batch_rowshard", "llvq_gemm_small_batch_sorted_rowshard",
     "llvq_sort_blocks_gemm_sg", "llvq_gemm_small_batch_sorted_sg",
     "llvq_gemv_multi", "llvq_gemv_sorted_multi",
-    "llvq_device", "llvq_mx_code_pitch", "llvq_mx_scale_pitch", "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_gemm_small_batch",
+    "llvq_device", "llvq_mx_code_pitch", "llvq_mx_scale_pitch", "llvq_mx_quantize", "llvq_mx_dequant_matrix", "llvq_mx_gemv", "llvq_mx_small_batch_bytes", "llvq_mx_gemm_small_batch",
     "llvq_mx_gemm", "llvq_embed", "llvq_mx_embed", "llvq_embed_grad_bytes", "llvq_embed_grad",
 ]
 
@@ -137,7 +137,9 @@ def load_library() -> ctypes.CDLL:
     lib.llvq_mx_quantize.argtypes = [vp, vp, ctypes.c_int, i64, i64, i64, vp, vp, vp]
     lib.llvq_mx_dequant_matrix.argtypes = [vp, vp, vp, i64, i64, vp, i64, vp]
     lib.llvq_mx_gemv.argtypes = [vp, vp, vp, i64, i64, vp, vp, ctypes.c_int, vp]
-    lib.llvq_mx_gemm_small_batch.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp]
+    lib.llvq_mx_small_batch_bytes.argtypes = [vp, i64, i64, ctypes.c_int]
+    lib.llvq_mx_small_batch_bytes.restype = ctypes.c_size_t
+    lib.llvq_mx_gemm_small_batch.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, vp, vp, vp]
     lib.llvq_mx_gemm.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, vp, vp]
     lib.llvq_embed.argtypes = [vp, vp, ctypes.c_int, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]
     lib.llvq_mx_embed.argtypes = [vp, vp, vp, i64, i64, vp, ctypes.c_int, i64, ctypes.c_float, vp, vp]

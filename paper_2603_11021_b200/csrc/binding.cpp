@@ -450,6 +450,16 @@ const void* token_args(Args& A, const llvq_ctx* ctx, const at::Tensor* t, int* b
     return on_device(A, ctx, t, "d_tokens");
 }
 
+// A call's own device memory, from PyTorch's allocator.  On a stream that is not the current one (`other`) it is marked as in use there, so that
+// it is not given away before the call is done.
+at::Tensor workspace(size_t bytes, const at::Tensor& like, bool other, void* stream)
+{
+    at::Tensor t = new_tensor({(int64_t)bytes}, at::kByte, like);
+    if (other && bytes > 0)
+        c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
+    return t;
+}
+
 double real(Args& A, int i)
 {
     if (!A.ok) return 0.0;
@@ -548,7 +558,9 @@ LLVQ_FUNC(mx_gemm_small, 8)
     uint16_t* py = static_cast<uint16_t*>(on_device(A, ctx, &y, "d_y"));
     void* st = stream_of(A, 7, *c);
     if (!A.ok) return nullptr;
-    const int r = call([&] { return llvq_mx_gemm_small_batch(ctx, m.codes, m.scales, n_out, k_in, px, (int)batch, py, st); });
+    const at::Tensor work = workspace(llvq_mx_small_batch_bytes(ctx, n_out, k_in, (int)batch), *c, A.a[7] != Py_None, st);
+    void* pw = work.numel() ? work.data_ptr() : nullptr;
+    const int r = call([&] { return llvq_mx_gemm_small_batch(ctx, m.codes, m.scales, n_out, k_in, px, (int)batch, py, pw, st); });
     return result(r, std::move(y));
 }
 
@@ -645,10 +657,7 @@ LLVQ_FUNC(embed_grad, 10)
     const void *pt = token_args(A, ctx, t, &bytes), *pd = on_device(A, ctx, dy, "d_dy");
     void *pg = on_device(A, ctx, &g, "d_grad"), *st = stream_of(A, 9, *dy);
     if (!A.ok) return nullptr;
-    // The call's own lists and sums, from PyTorch's allocator: on a stream that is not the current one the memory is marked as in use there.
-    const at::Tensor work = new_tensor({(int64_t)llvq_embed_grad_bytes(n, dim)}, at::kByte, *dy);
-    if (A.a[9] != Py_None && work.numel() > 0)
-        c10::cuda::CUDACachingAllocator::recordStream(work.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), dy->device().index()));
+    const at::Tensor work = workspace(llvq_embed_grad_bytes(n, dim), *dy, A.a[9] != Py_None, st);
     const int r = call([&] {
         return llvq_embed_grad(ctx, pd, type, pt, bytes, n, vocab, dim, (float)scale, padding, accumulate, pg, grad_type, work.numel() ? work.data_ptr() : nullptr, st);
     });

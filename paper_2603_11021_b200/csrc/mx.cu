@@ -3,8 +3,8 @@
 #include <type_traits>
 
 #include "kernels_common.cuh"
-#include "mx.cuh"
-#include "umma.cuh"
+#include "mx_batch.h"
+#include "mx_tensor.cuh"
 
 namespace {
 
@@ -119,9 +119,9 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t 
 // what hides the latency of HBM, which bounds the kernel up to about 24 rows of X (4.25 bits per weight, read once); beyond, the products do.
 constexpr int kChunk = 512;                              // columns of a warp's part of a stage
 constexpr int kXWarps = 4;
-constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice
-template <int kWarps> struct Stream {                    // kWarps multiply
-    static constexpr int kThreads = (kWarps + 1 + kXWarps) * 32;
+constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice; the exponent is behind the columns
+template <int kWarps, bool kPre> struct Stream {         // kWarps multiply; kPre: X comes as mx_stream_split_kernel left it
+    static constexpr int kThreads = (kWarps + 1 + (kPre ? 1 : kXWarps)) * 32;
     static constexpr uint32_t kCodes = kWarps * 16 * (kChunk / 2), kScales = kWarps * 16 * 16;      // bytes per stage, whatever RG and KG
 };
 constexpr size_t kStreamSmem = 227 * 1024 - 1024;        // dynamic shared memory that a launch may use
@@ -131,6 +131,7 @@ struct MxStream {
     uint32_t kb, chunks, tiles;                          // blocks per row, chunks of 512 columns, tiles of 16 RG rows
     const __nv_bfloat16* x;
     int batch, x_align;                                  // rows of X; elements of X that one load may take: 8, 4, 2 or 1
+    uint8_t* x_chunks;                                   // X as binary16 in global memory (several rows), see mx_stream_split_kernel
     int rg_log2, stages;
     uint32_t stage_bytes, part_at;                       // of a stage; where the sums of warps that share rows are (KG > 1)
     void* y;
@@ -211,6 +212,39 @@ __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor)
     return f16_pair(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
 }
 
+// The 512 columns of a chunk of a row of X as they were loaded (columns 8 lane .. and 256 + 8 lane ..) to binary16, in place; the exponent of the factor.
+__device__ __forceinline__ int chunk_to_f16(uint4 v[2])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) m = max_finite(max_finite(max_finite(max_finite(m, v[h].x), v[h].y), v[h].z), v[h].w);
+    m = __reduce_max_sync(0xffffffffu, m);
+    const int f = min(14 - ((int)(m >> 7) - 127), 127);
+    const float factor = __uint_as_float((uint32_t)(f + 127) << 23);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h] = make_uint4(to_f16(v[h].x, factor), to_f16(v[h].y, factor), to_f16(v[h].z, factor), to_f16(v[h].w, factor));
+    return f;
+}
+
+// Several rows of X, once for all thread blocks: [chunk][row][kXPitch bytes], a warp per row and chunk.
+__global__ void __launch_bounds__(256)
+mx_stream_split_kernel(MxStream a)
+{
+    pdl_wait();
+    pdl_launch_dependents();                             // behind the wait: what the next kernel reads ahead of its own was written before this one
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * 8u + (threadIdx.x >> 5), chunk = unit / (uint32_t)a.batch;
+    if (chunk >= a.chunks) return;
+    const int n = (int)(unit - chunk * (uint32_t)a.batch);
+    const int64_t k = (int64_t)chunk * kChunk + lane * 8;
+    uint4 v[2] = {load_x8(a, n, k), load_x8(a, n, k + 256)};
+    const int f = chunk_to_f16(v);
+    uint8_t* to = a.x_chunks + (uint64_t)unit * kXPitch;
+    *reinterpret_cast<uint4*>(to + lane * 16) = v[0];
+    *reinterpret_cast<uint4*>(to + 512 + lane * 16) = v[1];
+    if (lane == 0) *reinterpret_cast<int*>(to + 1024) = f;
+}
+
 // d * 2^h in two steps, for h that binary32 may not hold; NaN for the scale byte 255
 __device__ __forceinline__ float scale_far(float d, uint32_t e, int f)
 {
@@ -219,25 +253,25 @@ __device__ __forceinline__ float scale_far(float d, uint32_t e, int f)
     return d * s1 * __uint_as_float((uint32_t)(h2 + 127) << 23);
 }
 
-template <int kWarps, int kTiles, bool kF32>
-__global__ void __launch_bounds__(Stream<kWarps>::kThreads, 1)
+template <int kWarps, int kTiles, bool kF32, bool kPre>
+__global__ void __launch_bounds__(Stream<kWarps, kPre>::kThreads, 1)
 mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constant__ CUtensorMap scales, MxStream a)
 {
-    constexpr uint32_t kCodes = Stream<kWarps>::kCodes, kScales = Stream<kWarps>::kScales;
+    constexpr uint32_t kCodes = Stream<kWarps, kPre>::kCodes, kScales = Stream<kWarps, kPre>::kScales;
     extern __shared__ uint8_t st_smem[];
     __shared__ uint64_t full[8], empty[8];
     const uint32_t base = (smem_u32(st_smem) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rg_n = 1 << a.rg_log2, kg_n = kWarps >> a.rg_log2;
     const uint32_t rows = 16u << a.rg_log2, steps = (a.chunks + kg_n - 1) / kg_n;      // steps: stages per tile
-    const uint32_t x_at = kCodes + kScales, f_at = x_at + kg_n * a.batch * kXPitch;      // inside a stage
+    constexpr uint32_t x_at = kCodes + kScales;          // inside a stage
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < a.stages; ++s) { mbar_init(full + s, 1 + kXWarps); mbar_init(empty + s, kWarps); }
+        for (int s = 0; s < a.stages; ++s) { mbar_init(full + s, kPre ? 2 : 1 + kXWarps); mbar_init(empty + s, kWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    pdl_wait();
+    if (!kPre) pdl_wait();                               // else the warp of X waits, and nothing is written before X has come
     bool ok = true;
     uint32_t s = 0, phase = 0;                           // stage and its phase
     auto next = [&] { if (++s == (uint32_t)a.stages) { s = 0; phase ^= 1u; } };
@@ -256,6 +290,21 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                         tma_load_2d(at + g * rows * (kChunk / 2) + rows * 128u, &codes, chunk * (kChunk / 2) + 128, (int)(tile * rows), full + s);
                         tma_load_2d(at + kCodes + g * rows * 16u, &scales, chunk * 16, (int)(tile * rows), full + s);
                     }
+                    next();
+                }
+            }
+        }
+    } else if (kPre && warp > kWarps) {
+        if (lane == 0) {
+            pdl_wait();
+            uint32_t it = 0;
+            for (uint32_t tile = blockIdx.x; tile < a.tiles && ok; tile += gridDim.x) {
+                for (uint32_t step = 0; step < steps; ++step, ++it) {
+                    if (it >= (uint32_t)a.stages) ok = mbar_wait(empty + s, phase ^ 1u);
+                    if (!ok) break;
+                    const uint32_t chunk = step * kg_n, count = min((uint32_t)kg_n, a.chunks - chunk), bytes = count * a.batch * kXPitch;
+                    mbar_expect(full + s, bytes);
+                    bulk_load(base + s * a.stage_bytes + x_at, a.x_chunks + (uint64_t)chunk * a.batch * kXPitch, bytes, full + s);
                     next();
                 }
             }
@@ -281,17 +330,11 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                     for (int u = 0; u < kAhead; ++u) {
                         const int i = i0 + u * kXWarps;
                         if (i >= items) break;           // the same for the whole warp
-                        uint32_t m = 0;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) m = max_finite(max_finite(max_finite(max_finite(m, v[u][h].x), v[u][h].y), v[u][h].z), v[u][h].w);
-                        m = __reduce_max_sync(0xffffffffu, m);
-                        const int f = min(14 - ((int)(m >> 7) - 127), 127);
-                        const float factor = __uint_as_float((uint32_t)(f + 127) << 23);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            sts128(at + x_at + i * kXPitch + h * 512u + lane * 16u,
-                                   make_uint4(to_f16(v[u][h].x, factor), to_f16(v[u][h].y, factor), to_f16(v[u][h].z, factor), to_f16(v[u][h].w, factor)));
-                        if (lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + f_at + i * 4u), "r"(f) : "memory");
+                        const int f = chunk_to_f16(v[u]);
+                        const uint32_t to = at + x_at + i * kXPitch;
+                        sts128(to + lane * 16u, v[u][0]);
+                        sts128(to + 512u + lane * 16u, v[u][1]);
+                        if (lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 1024u), "r"(f) : "memory");
                     }
                 }
                 __syncwarp();
@@ -334,7 +377,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            f[n][c] = (int)lds32(at + f_at + (kg * a.batch + min(n * 8 + 2 * t + c, a.batch - 1)) * 4u);
+                            f[n][c] = (int)lds32(at + x_at + (kg * a.batch + min(n * 8 + 2 * t + c, a.batch - 1)) * kXPitch + 1024u);
                             near &= f[n][c] >= -30 && f[n][c] <= 50;
                         }
                     const uint32_t codes_at = (at + row_at) | ((mblock ^ swizzle) << 4), x_row = at + x_at + kg * a.batch * kXPitch + t * 16u;
@@ -427,20 +470,6 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
     if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
 }
 
-// A tensor map of rows of bytes: boxes of `width` bytes by `box` rows.  (The driver's function asks for a current context: see make_x_map.)
-bool make_byte_map(int device, const uint8_t* p, int64_t pitch, int64_t rows, int width, int box, bool swizzle, CUtensorMap* map)
-{
-    const EncodeTiled encode = encode_tiled();
-    if (!encode) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t size[2] = {(cuuint32_t)width, (cuuint32_t)box}, steps[2] = {1, 1};
-    auto made = [&] {
-        return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, size, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    };
-    return made() || (cudaSetDevice(device) == cudaSuccess && made());
-}
-
 // Sizes whose byte counts leave 63 bits, or dimensions that the kernels' indices do not hold.
 bool mx_too_large(int64_t rows, int64_t cols) { return rows > (1ll << 31) || cols > (1ll << 31); }
 
@@ -461,42 +490,39 @@ cudaError_t launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t l
     return launch_pdl(mx_quantize_kernel<T>, (unsigned)ctas, kMxThreads, 0, st, static_cast<const T*>(x), rows, cols, ld, pieces, wide, codes, scales);
 }
 
-template <int kWarps, int kTiles>
-int launch_stream(const llvq_ctx* ctx, const CUtensorMap& codes, const CUtensorMap& scales, const MxStream& a, unsigned grid, size_t smem, int y_dtype, cudaStream_t st)
+template <int kWarps, int kTiles, bool kF32, bool kPre>
+int launch_stream(const llvq_ctx* ctx, const CUtensorMap& codes, const CUtensorMap& scales, const MxStream& a, unsigned grid, size_t smem, cudaStream_t st)
 {
-    cudaError_t r;
-    if (y_dtype == LLVQ_F32) {
-        if (!set_smem<mx_stream_kernel<kWarps, kTiles, true>>(ctx, smem)) return LLVQ_ECUDA;
-        r = launch_pdl(mx_stream_kernel<kWarps, kTiles, true>, grid, Stream<kWarps>::kThreads, smem, st, codes, scales, a);
-    } else {
-        if (!set_smem<mx_stream_kernel<kWarps, kTiles, false>>(ctx, smem)) return LLVQ_ECUDA;
-        r = launch_pdl(mx_stream_kernel<kWarps, kTiles, false>, grid, Stream<kWarps>::kThreads, smem, st, codes, scales, a);
-    }
+    if (!set_smem<mx_stream_kernel<kWarps, kTiles, kF32, kPre>>(ctx, smem)) return LLVQ_ECUDA;
+    const cudaError_t r = launch_pdl(mx_stream_kernel<kWarps, kTiles, kF32, kPre>, grid, Stream<kWarps, kPre>::kThreads, smem, st, codes, scales, a);
     return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
-int mx_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x, int batch, void* d_y,
-               int y_dtype, cudaStream_t st)
+constexpr int kStreamBatch = 16;                         // rows of X up to which weights go through registers; beyond, mx_batch_product
+
+uint64_t stream_x_bytes(int64_t k_in, int batch) { return (uint64_t)(k_in + kChunk - 1) / kChunk * (uint64_t)batch * kXPitch; }
+
+// batch up to kStreamBatch; work: stream_x_bytes() of device memory for more than one row
+int mx_stream_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x, int batch,
+                      void* d_y, int y_dtype, uint8_t* work, cudaStream_t st)
 {
-    DeviceGuard guard(ctx->device);
-    if (!guard.ok) return LLVQ_ECUDA;
-    if (k_in == 0) return cudaMemsetAsync(d_y, 0, (size_t)n_out * batch * (y_dtype == LLVQ_F32 ? 4 : 2), st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
     MxStream a{};
     a.n_out = n_out; a.k_in = k_in; a.kb = (uint32_t)mx_blocks(k_in); a.chunks = (a.kb + 15) / 16;
-    a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y; a.flags = ctx->dev.flags;
+    a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y; a.flags = ctx->dev.flags; a.x_chunks = work;
     a.x_align = 8;
     while (a.x_align > 1 && (!aligned(d_x, 2 * (size_t)a.x_align) || (batch > 1 && k_in % a.x_align != 0))) a.x_align /= 2;
-    const int tiles = (batch + 7) / 8, kept = tiles <= 4 ? tiles : 8, warps = tiles <= 2 ? 16 : 8, most = warps == 16 ? 4 : 3;
-    const uint32_t fixed = warps == 16 ? Stream<16>::kCodes + Stream<16>::kScales : Stream<8>::kCodes + Stream<8>::kScales;
+    constexpr int kWarps = 16;
+    const int tiles = (batch + 7) / 8;
+    constexpr uint32_t fixed = Stream<kWarps, true>::kCodes + Stream<kWarps, true>::kScales;
     // Rows of a tile: what takes the fewest rounds over the SMs, counted in rows, with a quarter of the smallest tile on top for the end of a tile,
     // no more warps along a row than it has chunks, and two stages at least.
     uint64_t best = ~0ull;
     size_t smem = 0;
-    for (int l = most; l >= 0; --l) {
-        const int kg = warps >> l;
-        if (l < most && kg / 2 >= (int)a.chunks) break;
-        const uint32_t stage = (fixed + (uint32_t)(kg * batch) * (kXPitch + 4u) + 1023u) & ~1023u;
-        const uint32_t part = kg > 1 ? (uint32_t)kg * kept * 8u * (16u << l) * 4u : 0u;
+    for (int l = 4; l >= 0; --l) {
+        const int kg = kWarps >> l;
+        if (l < 4 && kg / 2 >= (int)a.chunks) break;
+        const uint32_t stage = (fixed + (uint32_t)(kg * batch) * kXPitch + 1023u) & ~1023u;
+        const uint32_t part = kg > 1 ? (uint32_t)kg * tiles * 8u * (16u << l) * 4u : 0u;
         const int stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / stage);
         if (stages < 2) continue;
         const uint64_t count = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), cost = (count + ctx->sm_count - 1) / ctx->sm_count * ((4u << l) + 1u);
@@ -510,13 +536,14 @@ int mx_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_sca
     if (!make_byte_map(ctx->device, d_codes, mx_code_pitch(k_in), n_out, 128, 16 << a.rg_log2, true, &codes) ||
         !make_byte_map(ctx->device, d_scales, mx_scale_pitch(k_in), n_out, 16, 16 << a.rg_log2, false, &scales)) return LLVQ_ECUDA;
     const unsigned grid = std::min<unsigned>(a.tiles, (unsigned)ctx->sm_count);
-    switch (kept) {
-        case 1: return launch_stream<16, 1>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 2: return launch_stream<16, 2>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 3: return launch_stream<8, 3>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        case 4: return launch_stream<8, 4>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-        default: return launch_stream<8, 8>(ctx, codes, scales, a, grid, smem, y_dtype, st);
-    }
+    if (batch == 1)
+        return y_dtype == LLVQ_F32 ? launch_stream<kWarps, 1, true, false>(ctx, codes, scales, a, grid, smem, st)
+                                   : launch_stream<kWarps, 1, false, false>(ctx, codes, scales, a, grid, smem, st);
+    const uint64_t split = ((uint64_t)a.chunks * batch + 7) / 8;
+    if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
+    if (launch_pdl(mx_stream_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
+    return tiles == 1 ? launch_stream<kWarps, 1, false, true>(ctx, codes, scales, a, grid, smem, st)
+                      : launch_stream<kWarps, 2, false, true>(ctx, codes, scales, a, grid, smem, st);
 }
 
 }  // namespace
@@ -552,18 +579,34 @@ int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_s
     if ((!d_x_bf16 && k_in != 0) || !d_y || n_out < 0 || k_in < 0 || (y_dtype != LLVQ_F32 && y_dtype != LLVQ_BF16)) return LLVQ_EINVAL;
     if (!aligned(d_x_bf16, 2) || !aligned(d_y, y_dtype == LLVQ_F32 ? 4 : 2)) return LLVQ_EALIGN;
     if (n_out > (1ll << 30) || k_in > (1ll << 30)) return LLVQ_EUNSUPPORTED;      // TMA coordinates
-    return mx_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, 1, d_y, y_dtype, (cudaStream_t)stream);
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return LLVQ_ECUDA;
+    if (k_in == 0) return cudaMemsetAsync(d_y, 0, (size_t)n_out * (y_dtype == LLVQ_F32 ? 4 : 2), (cudaStream_t)stream) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
+    return mx_stream_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, 1, d_y, y_dtype, nullptr, (cudaStream_t)stream);
+}
+
+size_t llvq_mx_small_batch_bytes(const llvq_ctx* ctx, int64_t n_out, int64_t k_in, int batch)
+{
+    if (!ctx || ctx->device < 0 || n_out <= 0 || k_in <= 0 || batch <= 0 || batch > 64 || n_out > (1ll << 30) || k_in > (1ll << 30)) return 0;
+    return batch == 1 ? 0 : batch <= kStreamBatch ? (size_t)stream_x_bytes(k_in, batch) : mx_batch_bytes(ctx, n_out, k_in, batch);
 }
 
 int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x_bf16,
-                             int batch, uint16_t* d_y_bf16, void* stream)
+                             int batch, uint16_t* d_y_bf16, void* d_work, void* stream)
 {
     if (ctx && ctx->device >= 0 && (n_out == 0 || batch == 0)) return LLVQ_OK;
     if (int e = mx_check(ctx, k_in == 0, d_codes, d_scales)) return e;
     if ((!d_x_bf16 && k_in != 0) || !d_y_bf16 || n_out < 0 || k_in < 0 || batch < 0) return LLVQ_EINVAL;
-    if (!aligned(d_x_bf16, 2) || !aligned(d_y_bf16, 2)) return LLVQ_EALIGN;
+    if (!aligned(d_x_bf16, 2) || !aligned(d_y_bf16, 2) || !aligned(d_work, 256)) return LLVQ_EALIGN;
     if (batch > 64 || n_out > (1ll << 30) || k_in > (1ll << 30)) return LLVQ_EUNSUPPORTED;
-    return mx_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, LLVQ_BF16, (cudaStream_t)stream);
+    if (batch > 1 && k_in > 0 && !d_work) return LLVQ_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return LLVQ_ECUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (k_in == 0) return cudaMemsetAsync(d_y_bf16, 0, (size_t)n_out * batch * 2, st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
+    uint8_t* work = static_cast<uint8_t*>(d_work);
+    return batch <= kStreamBatch ? mx_stream_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, LLVQ_BF16, work, st)
+                                 : mx_batch_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, work, st);
 }
 
 }  // extern "C"

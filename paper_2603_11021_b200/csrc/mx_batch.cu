@@ -1,0 +1,403 @@
+// Product of a microscaled 4-bit matrix with 2 to 64 rows of bf16 activations on the tensor cores' block-scaled instruction
+// (see include/llvq.h and mx.cuh).
+#include "kernels_common.cuh"
+#include "mx_tensor.cuh"
+#include "mx_batch.h"
+
+namespace {
+
+using namespace llvq;
+
+// tcgen05.mma.kind::mxf8f6f4 multiplies e2m1 with e4m3, each with a power of two per row and 32 columns, so W goes to the tensor cores as it is stored
+// and no weight passes through a register.  A bf16 number is three e4m3 numbers: with s = 2^(E - 7), E the exponent of the largest finite
+// magnitude of the 32 columns,
+//     x = s q1 + 2^-5 s q2 + 2^-23 s q3,   q1 = rn(x / s),  q2 = rn of 2^5 times what is left,  q3 = rn of 2^23 times what is left then.
+// |x / s| < 256; q1 and q2 take four significant bits each, which is all of a bf16 number down to 2^-14 of the block's largest; with q3 it is exact
+// down to 2^-19 of it, and what is smaller is off by at most 2^-27 of it, below the rounding of a sum in binary32 that holds the largest.
+// A row of X is three columns of the product, added up in binary32 at the end.
+//
+// First kernel: the three terms of X, laid out as the second copies them (chunks of 128 columns: rows of 128 bytes, swizzled, then their scales),
+// once for all thread blocks.  Second kernel: tiles of 128 rows of W by all of X.  The steps of 128 columns of all tiles are dealt out evenly in one
+// line, so every SM reads the same share of W whatever the shape; a tile that several thread blocks share is added up by whichever
+// is done last, in the order of the blocks.
+//   warps 4-7   copy codes with cp.async, 8 bytes (16 elements) into every 16 of shared memory: the form in which the instruction takes 4-bit operands
+//   warp 8      the scales of W    warp 9: X    warp 10: the MMAs, four per stage    warps 0-3: the accumulator and Y
+// It begins to read W while the first kernel still runs (which waits for everything before it first).
+// Bound by HBM for few rows of X; at 64 the products take as long as the reads.
+constexpr int kBatchRows = 128, kBatchCols = 128, kBatchThreads = 352;
+constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a stage's weights, a byte of room per element
+
+__host__ __device__ inline uint32_t batch_npad(int batch) { return (3u * (uint32_t)batch + 15u) / 16u * 16u; }
+__host__ __device__ inline uint32_t batch_x_bytes(uint32_t npad) { return npad * 128u + 2u * kScaleAtom; }      // of a chunk
+
+// The workspace: X in chunks, a counter per tile, a byte per chunk and row of X (not finite), sums of tiles that are shared (two per thread block).
+struct BatchWork {
+    uint64_t x, counters, notes, parts, bytes;
+};
+__host__ __device__ inline uint64_t up256(uint64_t v) { return (v + 255) / 256 * 256; }
+BatchWork batch_work(int64_t n_out, int64_t k_in, int batch, int sms)
+{
+    const uint64_t chunks = (uint64_t)(k_in + kBatchCols - 1) / kBatchCols, tiles = (uint64_t)(n_out + kBatchRows - 1) / kBatchRows;
+    BatchWork w;
+    w.x = 0;
+    w.counters = up256(chunks * batch_x_bytes(batch_npad(batch)));
+    w.notes = w.counters + up256(tiles * 4);
+    w.parts = w.notes + up256(chunks * batch);
+    w.bytes = w.parts + (uint64_t)sms * 2 * kBatchRows * batch * 4;
+    return w;
+}
+
+struct BatchArgs {
+    const uint8_t *codes, *scales;
+    int64_t n_out, k_in, code_pitch;
+    uint32_t kb, scale_pitch, steps, tiles;               // blocks per row; steps of 128 columns per tile
+    const __nv_bfloat16* x;
+    int batch;
+    bool x_quads;                                         // four elements of X may be loaded at once
+    uint32_t npad;
+    uint8_t* x_chunks;
+    uint32_t* counters;
+    uint8_t* notes;
+    float* parts;
+    __nv_bfloat16* y;
+    uint32_t* flags;
+};
+
+__device__ __forceinline__ uint32_t e4m3x4(const float v[4])
+{
+    uint32_t r;
+    asm("{\n .reg .b16 lo, hi;\n cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n mov.b32 %0, {lo, hi};\n}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+    return r;
+}
+
+__device__ __forceinline__ void e4m3x4_values(uint32_t w, float v[4])
+{
+    uint32_t a, b;
+    asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %2;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n cvt.rn.f16x2.e4m3x2 %1, hi;\n}" : "=r"(a), "=r"(b) : "r"(w));
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&a)), q = __half22float2(*reinterpret_cast<const __half2*>(&b));
+    v[0] = p.x; v[1] = p.y; v[2] = q.x; v[3] = q.y;
+}
+
+// A warp per row of X and chunk of 128 columns, four columns per lane.
+__global__ void __launch_bounds__(256)
+mx_batch_split_kernel(BatchArgs a)
+{
+    pdl_wait();
+    pdl_launch_dependents();                              // behind the wait: what the next kernel reads ahead of its own was written before this one
+    const int lane = threadIdx.x & 31;
+    const uint32_t unit = blockIdx.x * 8u + (threadIdx.x >> 5);
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < a.tiles; i += gridDim.x * 256u) a.counters[i] = 0u;
+    if (unit >= a.steps * (uint32_t)a.batch) return;
+    const uint32_t chunk = unit / (uint32_t)a.batch, n = unit - chunk * (uint32_t)a.batch;
+    const int64_t k = (int64_t)chunk * kBatchCols + lane * 4;
+    const __nv_bfloat16* p = a.x + (int64_t)n * a.k_in + k;
+    uint32_t w[2] = {0u, 0u};
+    if (a.x_quads && k + 4 <= a.k_in) {
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = u.x; w[1] = u.y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (k + j < a.k_in) w[j >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short*>(p) + j) << (16 * (j & 1));
+    }
+    float v[4];
+    uint32_t most = 0, note = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t bits = (w[j >> 1] >> (16 * (j & 1))) & 0xffffu, size = bits & 0x7fffu;
+        v[j] = __uint_as_float(bits << 16);
+        if (size < 0x7f80u) most = max(most, size);
+        else note |= size == 0x7f80u ? 1u : 2u;
+        if (size >= 0x7f80u) v[j] = __uint_as_float(0x7fc00000u);        // no infinity in e4m3: the row's results are NaN, which mx_batch_kernel looks into
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const uint32_t any = __any_sync(0xffffffffu, note & 2u) ? 2u : __any_sync(0xffffffffu, note & 1u) ? 1u : 0u;
+    if (lane == 0) a.notes[(uint64_t)chunk * a.batch + n] = (uint8_t)any;
+    uint8_t* to = a.x_chunks + (uint64_t)chunk * batch_x_bytes(a.npad);
+    uint8_t* scales = to + a.npad * 128u;
+    const int s1 = max((int)(most >> 7) - 7, 0);
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {
+        const int s = max(s1 - (term == 0 ? 0 : term == 1 ? 5 : 23), 0);
+        const float up = __uint_as_float((uint32_t)(254 - s) << 23), down = mx_scale_value((uint32_t)s);      // s <= 247
+        const uint32_t row = 3u * n + term;
+        float q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = v[j] * up;
+        const uint32_t packed = e4m3x4(q);
+        *reinterpret_cast<uint32_t*>(to + row * 128u + ((((uint32_t)lane >> 2) ^ (row & 7u)) << 4) + (lane & 3u) * 4u) = packed;
+        if ((lane & 7) == 0) scales[(row >> 7) * kScaleAtom + (row & 31u) * 16u + ((row & 127u) >> 5) * 4u + (lane >> 3)] = (uint8_t)s;
+        e4m3x4_values(packed, q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] -= q[j] * down;
+    }
+    if (n == 0) {                                         // rows that fill up the tile
+        for (uint32_t row = 3u * a.batch; row < a.npad; ++row) {
+            *reinterpret_cast<uint32_t*>(to + row * 128u + lane * 4u) = 0u;
+            if (lane == 0) *reinterpret_cast<uint32_t*>(scales + (row >> 7) * kScaleAtom + (row & 31u) * 16u + ((row & 127u) >> 5) * 4u) = 0u;
+        }
+    }
+}
+
+// e2m1 (A) x e4m3 (B) with e8m0 scales, byte `id` of the words of scales -> f32, both operands K-major, M = 128, N = n
+__device__ __forceinline__ uint32_t instr_desc_mxf4_f8(uint32_t n, uint32_t id)
+{
+    return id << 4 | 5u << 7 | 0u << 10 | (n >> 3) << 17 | 1u << 23 | (128u >> 4) << 24 | id << 29;
+}
+
+__device__ __forceinline__ void umma_mxf8f6f4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scales, uint32_t b_scales, uint32_t accumulate)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory"); }
+
+// The share of thread block i of `blocks`: steps [i * units / blocks, (i + 1) * units / blocks) of all tiles in one line.
+__device__ __forceinline__ uint64_t share_begin(uint64_t units, uint32_t blocks, uint32_t i) { return units * i / blocks; }
+__device__ __forceinline__ uint32_t share_owner(uint64_t units, uint32_t blocks, uint64_t u) { return (uint32_t)(((u + 1) * blocks - 1) / units); }
+
+// One result in binary32, product by product: for rows of X with an infinity, which the three terms cannot hold.
+__device__ __noinline__ float dot_plain(const BatchArgs& a, int64_t row, int n)
+{
+    float sum = 0.0f;
+    for (int64_t k = 0; k < a.k_in; ++k) {
+        const uint32_t byte = a.codes[row * a.code_pitch + (k >> 1)], e = a.scales[row * a.scale_pitch + (k >> 5)];
+        float v[8];
+        mx_expand8((byte >> (4 * (k & 1))) & 15u, v);
+        sum += v[0] * mx_scale_value(e) * __bfloat162float(a.x[(int64_t)n * a.k_in + k]);
+    }
+    return sum;
+}
+
+__device__ __forceinline__ void put_y(const BatchArgs& a, int64_t row, int n, float v)
+{
+    if (row >= a.n_out) return;
+    if (v != v) {                                         // NaN stays where X has one; else an infinity may be behind it
+        bool nan = false, inf = false;
+        for (uint32_t c = 0; c < a.steps; ++c) { const uint8_t note = a.notes[(uint64_t)c * a.batch + n]; nan |= note == 2; inf |= note == 1; }
+        if (inf && !nan) v = dot_plain(a, row, n);
+    }
+    a.y[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(v);
+}
+
+template <int kStages>
+__global__ void __launch_bounds__(kBatchThreads, 1)
+mx_batch_kernel(BatchArgs a)
+{
+    extern __shared__ uint8_t mb_smem[];
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full, acc_empty;
+    __shared__ uint32_t tmem_slot, last_slot;
+    const uint32_t base = (smem_u32(mb_smem) + 1023u) & ~1023u;
+    const uint32_t x_bytes = batch_x_bytes(a.npad), stage_bytes = (kBatchA + x_bytes + kScaleAtom + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint64_t units = (uint64_t)a.tiles * a.steps, begin = share_begin(units, gridDim.x, blockIdx.x), end = share_begin(units, gridDim.x, blockIdx.x + 1);
+
+    pdl_launch_dependents();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) { mbar_init(full + s, 128 + 2); mbar_init(empty + s, 1); }       // 128 threads' copies of codes, scales, X
+        mbar_init(&acc_full, 1);
+        mbar_init(&acc_empty, 4);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 10) tmem_alloc(&tmem_slot, 256);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    bool ok = true;
+    uint32_t s = 0, phase = 0;
+    auto next = [&] { if (++s == (uint32_t)kStages) { s = 0; phase ^= 1u; } };
+    uint32_t it = 0;                                      // stages so far
+
+    if (warp >= 4 && warp < 8) {
+        const uint32_t p = threadIdx.x - 128u, c = p & 7u, r = p >> 3;          // container of a row; rows r, r + 16, ...
+        const uint32_t to = base + r * 128u + ((c ^ (r & 7u)) << 4);
+        for (uint64_t u = begin; u < end && ok; ++u, ++it) {
+            const uint32_t tile = (uint32_t)(u / a.steps), step = (uint32_t)(u - (uint64_t)tile * a.steps);
+            if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
+            if (!ok) break;
+            const int64_t row = (int64_t)tile * kBatchRows + r;
+            const bool in = step * 4u + (c >> 1) < a.kb;
+            const uint8_t* from = a.codes + row * a.code_pitch + (uint64_t)step * 64u + c * 8u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool ok_row = in && row + 16 * i < a.n_out;
+                const uint8_t* src = ok_row ? from + (int64_t)(16 * i) * a.code_pitch : a.codes;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to + s * stage_bytes + i * 2048u), "l"(src), "r"(ok_row ? 8u : 0u) : "memory");
+            }
+            // counts on the stage's barrier once this thread's copies are there; the MMAs' thread makes them visible to the tensor cores
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full + s)) : "memory");
+            next();
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp == 8) {
+        ScaleQuad now, then;
+        uint32_t tile_of = 0xffffffffu, quad_of = 0;
+        for (uint64_t u = begin; u < end && ok; ++u, ++it) {
+            const uint32_t tile = (uint32_t)(u / a.steps), step = (uint32_t)(u - (uint64_t)tile * a.steps), quad = step / 4u;
+            if (tile != tile_of || quad != quad_of) {     // 16 scales of a row serve four steps; the next ones are requested when these come into use
+                if (tile == tile_of) now = then;
+                else load_scales(now, a.scales, (int64_t)tile * kBatchRows, a.n_out, a.scale_pitch, a.kb, quad, lane);
+                load_scales(then, a.scales, (int64_t)tile * kBatchRows, a.n_out, a.scale_pitch, a.kb, quad + 1, lane);
+                tile_of = tile; quad_of = quad;
+            }
+            if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
+            if (!ok) break;
+            const uint32_t at = base + s * stage_bytes + kBatchA + x_bytes;
+            switch (step & 3u) {
+                case 0: store_scales<0>(at, now, a.kb, quad * 16u, lane); break;
+                case 1: store_scales<1>(at, now, a.kb, quad * 16u, lane); break;
+                case 2: store_scales<2>(at, now, a.kb, quad * 16u, lane); break;
+                default: store_scales<3>(at, now, a.kb, quad * 16u, lane);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive(full + s);
+            next();
+        }
+    } else if (warp == 9) {
+        if (lane == 0) {
+            pdl_wait();
+            for (uint64_t u = begin; u < end && ok; ++u, ++it) {
+                if (it >= (uint32_t)kStages) ok = mbar_wait(empty + s, phase ^ 1u);
+                if (!ok) break;
+                mbar_expect(full + s, x_bytes);
+                bulk_load(base + s * stage_bytes + kBatchA, a.x_chunks + (u % a.steps) * x_bytes, x_bytes, full + s);
+                next();
+            }
+        }
+    } else if (warp == 10) {
+        if (lane == 0) {
+            uint32_t done = 0;
+            for (uint64_t u = begin; u < end && ok; ++done) {
+                const uint64_t stop = min(end, (u / a.steps + 1) * a.steps);
+                if (done > 0) ok = mbar_wait(&acc_empty, (done - 1u) & 1u);
+                tc_fence_after();
+                for (bool first = true; u < stop && ok; ++u, ++it, first = false) {
+                    ok = mbar_wait_copies(full + s, phase);
+                    if (!ok) break;
+                    fence_async_smem();                   // the codes were copied by the generic proxy
+                    tc_fence_after();
+                    const uint32_t at = base + s * stage_bytes, xb = at + kBatchA, sb = xb + a.npad * 128u, sa = xb + x_bytes;
+                    const uint32_t ta = tmem + 192u + (it & 1u) * 12u, tb = ta + 4u;
+                    scales_to_tmem(ta, sa);
+                    scales_to_tmem(tb, sb);
+                    if (a.npad > 128u) scales_to_tmem(tb + 4u, sb + kScaleAtom);
+                    const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(xb);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)           // 32 columns: 32 bytes on along the rows of either operand, the next byte of the scales
+                        umma_mxf8f6f4(tmem, da + 2 * q, db + 2 * q, instr_desc_mxf4_f8(a.npad, q), ta, tb, !first || q > 0);
+                    umma_commit(empty + s);
+                    next();
+                }
+                if (ok) umma_commit(&acc_full);
+            }
+        }
+    } else {
+        pdl_wait();
+        uint32_t done = 0;
+        for (uint64_t u = begin; u < end; ++done) {
+            const uint32_t tile = (uint32_t)(u / a.steps);
+            const uint64_t tile_begin = (uint64_t)tile * a.steps, stop = min(end, tile_begin + a.steps);
+            ok = __all_sync(0xffffffffu, mbar_wait_copies(&acc_full, done & 1u));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t from = share_owner(units, gridDim.x, tile_begin), to = share_owner(units, gridDim.x, tile_begin + a.steps - 1);
+            const bool whole = from == to;
+            const int r = warp * 32 + lane;
+            const int64_t row = (int64_t)tile * kBatchRows + r;
+            auto slot = [&](uint32_t block) {             // where a block's sums of this tile are: its first tile or its last
+                const bool first = (uint32_t)(share_begin(units, gridDim.x, block) / a.steps) == tile;
+                return a.parts + ((uint64_t)block * 2 + (first ? 0 : 1)) * (uint64_t)(kBatchRows * a.batch) + r;
+            };
+            float* part = slot(blockIdx.x);
+            for (int n0 = 0; n0 < a.batch; n0 += 16) {
+                float v[48];
+#pragma unroll
+                for (int h = 0; h < 3; ++h)
+                    if (3u * n0 + 16u * h < a.npad) tmem_ld16(tmem + ((uint32_t)warp << 21) + 3u * n0 + 16u * h, v + 16 * h);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (n0 + j >= a.batch) break;
+                    const float sum = v[3 * j] + (v[3 * j + 1] + v[3 * j + 2]);
+                    if (whole) put_y(a, row, n0 + j, sum);
+                    else __stcg(part + (n0 + j) * kBatchRows, sum);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive(&acc_empty);
+            if (!whole) {                                 // the last of the blocks that share the tile adds their sums up
+                __threadfence();
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                if (threadIdx.x == 0) last_slot = atomicAdd(a.counters + tile, 1u) == to - from;
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                const bool last = last_slot != 0u;
+                if (last) {
+                    __threadfence();
+                    // 16 rows of X at a time, so that their loads overlap
+                    for (int n0 = 0; n0 < a.batch; n0 += 16) {
+                        float sum[16] = {};
+#pragma unroll 2
+                        for (uint32_t b = from; b <= to; ++b) {
+                            const float* p = slot(b) + n0 * kBatchRows;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                if (n0 + j < a.batch) sum[j] += __ldcg(p + j * kBatchRows);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (n0 + j < a.batch) put_y(a, row, n0 + j, sum[j]);
+                    }
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            }
+            u = stop;
+        }
+    }
+    if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 10) tmem_dealloc(tmem, 256);
+}
+
+template <int kStages>
+int launch_batch(const llvq_ctx* ctx, const BatchArgs& a, unsigned grid, cudaStream_t st)
+{
+    const size_t smem = 1024 + (size_t)kStages * ((kBatchA + batch_x_bytes(a.npad) + kScaleAtom + 1023u) & ~1023u);
+    if (!set_smem<mx_batch_kernel<kStages>>(ctx, smem)) return LLVQ_ECUDA;
+    return launch_pdl(mx_batch_kernel<kStages>, grid, kBatchThreads, smem, st, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+}
+
+}  // namespace
+
+namespace llvq {
+
+size_t mx_batch_bytes(const llvq_ctx* ctx, int64_t n_out, int64_t k_in, int batch) { return (size_t)batch_work(n_out, k_in, batch, ctx->sm_count).bytes; }
+
+int mx_batch_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x, int batch,
+                     uint16_t* d_y, uint8_t* work, cudaStream_t st)
+{
+    BatchArgs a{};
+    a.codes = d_codes; a.scales = d_scales; a.n_out = n_out; a.k_in = k_in; a.code_pitch = mx_code_pitch(k_in); a.scale_pitch = (uint32_t)mx_scale_pitch(k_in);
+    a.kb = (uint32_t)mx_blocks(k_in); a.steps = (a.kb + 3) / 4; a.tiles = (uint32_t)((n_out + kBatchRows - 1) / kBatchRows);
+    a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.x_quads = aligned(d_x, 8) && (batch == 1 || k_in % 4 == 0);
+    a.npad = batch_npad(batch); a.y = reinterpret_cast<__nv_bfloat16*>(d_y); a.flags = ctx->dev.flags;
+    const BatchWork w = batch_work(n_out, k_in, batch, ctx->sm_count);
+    a.x_chunks = work + w.x; a.counters = reinterpret_cast<uint32_t*>(work + w.counters); a.notes = work + w.notes; a.parts = reinterpret_cast<float*>(work + w.parts);
+    const uint64_t split = ((uint64_t)a.steps * batch + 7) / 8;
+    if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
+    if (launch_pdl(mx_batch_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
+    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles * a.steps, (uint64_t)ctx->sm_count);
+    // as many stages as shared memory holds
+    if (a.npad <= 48) return launch_batch<9>(ctx, a, grid, st);
+    if (a.npad <= 96) return launch_batch<7>(ctx, a, grid, st);
+    return launch_batch<5>(ctx, a, grid, st);
+}
+
+}  // namespace llvq

@@ -1,8 +1,7 @@
 // Product of two matrices in microscaled 4-bit floating point on the tensor cores' own block-scaled instruction (see include/llvq.h and mx.cuh):
 // Y[t][i] = sum_k X[t][k] W[i][k], both operands as llvq_mx_quantize leaves them, sums in binary32, Y in bf16.
 #include "kernels_common.cuh"
-#include "mx.cuh"
-#include "umma.cuh"
+#include "mx_tensor.cuh"
 
 namespace {
 
@@ -21,7 +20,6 @@ constexpr int kMmThreads = 384;
 constexpr int kMmRows = 128;                              // rows of W per tile
 constexpr int kMmGroup = 16;                              // row tiles that are walked together, for L2
 constexpr uint32_t kStageCodes = 128;                     // bytes of a row's codes per stage: 256 columns
-constexpr uint32_t kScaleAtom = 512;                      // scales of 128 rows and 4 blocks
 
 template <int kBn> struct MmShape {
     static constexpr int kBHalves = kBn > 128 ? 2 : 1;    // groups of 128 tokens
@@ -56,12 +54,6 @@ __device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint
                  ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate) : "memory");
 }
 
-// 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t smem)
-{
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc(smem, 0u, 128u)) : "memory");
-}
-
 // 32 consecutive accumulator columns of this thread's lane, as pairs of bf16.
 __device__ __forceinline__ void tmem_ld32_bf16(uint32_t taddr, uint32_t v[16])
 {
@@ -83,31 +75,6 @@ __device__ __forceinline__ void mm_tile(const MmArgs& a, uint32_t tile, uint32_t
     const uint32_t high = min((uint32_t)kMmGroup, a.tiles_m - group * kMmGroup);
     n = in / high;
     m = group * kMmGroup + (in - n * high);
-}
-
-// 16 scales (blocks 16 p .. 16 p + 15) of the rows l, l + 32, l + 64, l + 96 of a group of 128 that starts at row0; zero outside the matrix.
-struct ScaleQuad { uint4 v[4]; };
-__device__ __forceinline__ void load_scales(ScaleQuad& q, const uint8_t* scales, int64_t row0, int64_t rows, uint32_t pitch, uint32_t kb, uint32_t p, int lane)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + lane + 32 * i;
-        q.v[i] = row < rows && 16u * p < kb ? __ldg(reinterpret_cast<const uint4*>(scales + row * pitch) + p) : make_uint4(0u, 0u, 0u, 0u);
-    }
-}
-
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
-
-// Words j and j + 1 of a quad to the two atoms of a stage; bytes of blocks past the row's last are zero.
-template <int j>
-__device__ __forceinline__ void store_scales(uint32_t smem, const ScaleQuad& q, uint32_t kb, uint32_t first_block, int lane)
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t b = first_block + 4u * (j + h), left = b < kb ? kb - b : 0u, keep = left >= 4u ? 0xffffffffu : (1u << (8u * left)) - 1u;
-        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(smem + h * kScaleAtom + lane * 16), "r"(word_of(q.v[0], j + h) & keep),
-                     "r"(word_of(q.v[1], j + h) & keep), "r"(word_of(q.v[2], j + h) & keep), "r"(word_of(q.v[3], j + h) & keep) : "memory");
-    }
 }
 
 template <int kBn>
@@ -210,9 +177,13 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
                     if (g > 0 && of_w) continue;
-                    if ((k & 1u) == 0u) store_scales<0>(at + 2 * g * kScaleAtom, now[g], a.kb, (k / 2) * 16u, lane);
-                    else {
-                        store_scales<2>(at + 2 * g * kScaleAtom, now[g], a.kb, (k / 2) * 16u, lane);
+                    const uint32_t to = at + 2 * g * kScaleAtom, first = (k / 2) * 16u;
+                    if ((k & 1u) == 0u) {
+                        store_scales<0>(to, now[g], a.kb, first, lane);
+                        store_scales<1>(to + kScaleAtom, now[g], a.kb, first, lane);
+                    } else {
+                        store_scales<2>(to, now[g], a.kb, first, lane);
+                        store_scales<3>(to + kScaleAtom, now[g], a.kb, first, lane);
                         now[g] = next[g];
                     }
                 }
@@ -253,25 +224,12 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     if (warp == 1) tmem_dealloc(tmem, S::kTmem);
 }
 
-// The tensor map of a matrix of codes: boxes of 128 bytes by `box` rows, 128-byte swizzle.  (The driver's function asks for a current context: see make_x_map.)
-bool make_code_map(int device, const uint8_t* codes, int64_t pitch, int64_t rows, int box, CUtensorMap* map)
-{
-    const EncodeTiled encode = encode_tiled();
-    if (!encode) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t size[2] = {kStageCodes, (cuuint32_t)box}, steps[2] = {1, 1};
-    auto made = [&] {
-        return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(codes), dims, strides, size, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-    };
-    return made() || (cudaSetDevice(device) == cudaSuccess && made());
-}
-
 template <int kBn>
 int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* w_codes, int64_t pitch, MmArgs a, cudaStream_t st)
 {
     CUtensorMap w_map, x_map;
-    if (!make_code_map(ctx->device, w_codes, pitch, a.n_out, kMmRows, &w_map) || !make_code_map(ctx->device, x_codes, pitch, a.tokens, kBn, &x_map)) return LLVQ_ECUDA;
+    if (!make_byte_map(ctx->device, w_codes, pitch, a.n_out, (int)kStageCodes, kMmRows, true, &w_map) ||
+        !make_byte_map(ctx->device, x_codes, pitch, a.tokens, (int)kStageCodes, kBn, true, &x_map)) return LLVQ_ECUDA;
     if (!set_smem<mx_gemm_kernel<kBn>>(ctx, MmShape<kBn>::kSmem)) return LLVQ_ECUDA;
     a.tiles_n = (uint32_t)((a.tokens + kBn - 1) / kBn);
     const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles_m * a.tiles_n, (uint64_t)ctx->sm_count);

@@ -1,0 +1,59 @@
+// What the kernels on microscaled 4-bit matrices share: tensor maps of byte rows, and scales on their way to tensor memory.
+#pragma once
+#include "launch_host.h"
+#include "mx.cuh"
+#include "umma.cuh"
+
+namespace llvq {
+
+constexpr uint32_t kScaleAtom = 512;                      // scales of 128 rows and 4 blocks: row r at 16 (r % 32) + 4 (r / 32), block j at byte j
+
+// 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t smem)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc(smem, 0u, 128u)) : "memory");
+}
+
+// 16 scales (blocks 16 p .. 16 p + 15) of the rows l, l + 32, l + 64, l + 96 of a group of 128 that starts at row0; zero outside the matrix.
+struct ScaleQuad { uint4 v[4]; };
+__device__ __forceinline__ void load_scales(ScaleQuad& q, const uint8_t* scales, int64_t row0, int64_t rows, uint32_t pitch, uint32_t kb, uint32_t p, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + lane + 32 * i;
+        q.v[i] = row < rows && 16u * p < kb ? __ldg(reinterpret_cast<const uint4*>(scales + row * pitch) + p) : make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+
+// Word j of a quad (blocks first_block + 4 j ...) as an atom of scales; bytes of blocks past the row's last are zero.
+template <int j>
+__device__ __forceinline__ void store_scales(uint32_t smem, const ScaleQuad& q, uint32_t kb, uint32_t first_block, int lane)
+{
+    const uint32_t b = first_block + 4u * j, left = b < kb ? kb - b : 0u, keep = left >= 4u ? 0xffffffffu : (1u << (8u * left)) - 1u;
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(smem + lane * 16), "r"(word_of(q.v[0], j) & keep), "r"(word_of(q.v[1], j) & keep),
+                 "r"(word_of(q.v[2], j) & keep), "r"(word_of(q.v[3], j) & keep) : "memory");
+}
+
+// `bytes` (a multiple of 16) from global to shared memory, both on 16-byte boundaries, counted on bar.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar)
+{
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+// A tensor map of rows of bytes: boxes of `width` bytes by `box` rows.  (The driver's function asks for a current context: see make_x_map.)
+inline bool make_byte_map(int device, const uint8_t* p, int64_t pitch, int64_t rows, int width, int box, bool swizzle, CUtensorMap* map)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t size[2] = {(cuuint32_t)width, (cuuint32_t)box}, steps[2] = {1, 1};
+    auto made = [&] {
+        return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, size, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                      swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    return made() || (cudaSetDevice(device) == cudaSuccess && made());
+}
+
+}  // namespace llvq

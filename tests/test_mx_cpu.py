@@ -51,7 +51,8 @@ def test_host_only_context_refuses_to_launch(P, ctx):
     assert L.llvq_mx_quantize(ctx._h, vp, 0, 1, 32, 32, vp, vp, None) == 1
     assert L.llvq_mx_dequant_matrix(ctx._h, vp, vp, 1, 32, vp, 32, None) == 1
     assert L.llvq_mx_gemv(ctx._h, vp, vp, 1, 32, vp, vp, 0, None) == 1
-    assert L.llvq_mx_gemm_small_batch(ctx._h, vp, vp, 1, 32, vp, 1, vp, None) == 1
+    assert L.llvq_mx_gemm_small_batch(ctx._h, vp, vp, 1, 32, vp, 1, vp, vp, None) == 1
+    assert L.llvq_mx_small_batch_bytes(ctx._h, 128, 128, 4) == 0 and L.llvq_mx_small_batch_bytes(None, 128, 128, 4) == 0
     assert L.llvq_mx_gemm(ctx._h, vp, vp, 1, vp, vp, 1, 32, vp, None) == 1
     assert L.llvq_embed(ctx._h, vp, 0, 1, 1, vp, 8, 1, 1.0, vp, None) == 1
     assert L.llvq_mx_embed(ctx._h, vp, vp, 1, 1, vp, 8, 1, 1.0, vp, None) == 1
