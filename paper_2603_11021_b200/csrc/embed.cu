@@ -10,9 +10,10 @@ namespace {
 using namespace llvq;
 
 // ---- lookup -------------------------------------------------------------------------------------------------------------------------
-// A thread writes 16 bytes of an output row at a time, on a 16-byte boundary whatever the row's own alignment; the elements that belong
-// there are taken out of the one or two aligned words of the source that hold them.  Bound by HBM (and by latency for few tokens): each row
-// is read and written once.  kRowUnits pieces per thread, all requested before the first is written.
+// A thread writes whole 16-byte pieces of an output row, on 16-byte boundaries whatever the row's own alignment; the elements that belong there
+// are taken out of the one or two aligned words of the source that hold them.  A group of lanes (32, or as many as a short row has pieces) takes
+// kRowUnits pieces per lane of one row, all requested before the first is written, so that row, token and addresses are worked out once for them.
+// Bound by HBM (and by latency for few tokens): each row is read and written once.
 constexpr int kRowThreads = 256, kRowUnits = 4;
 
 struct Rows {
@@ -24,7 +25,8 @@ struct Rows {
     int token_bytes;
     uint8_t* out;
     float scale;
-    uint32_t units, magic;              // pieces per output row, floor(2^32 / units)
+    uint32_t units, parts;              // pieces per output row; parts of kRowUnits pieces per lane that they make
+    int lanes_log2;                     // lanes of a group
     unsigned long long* bad_index;
 };
 
@@ -66,16 +68,15 @@ template <> __device__ __forceinline__ __nv_bfloat16 scaled(__nv_bfloat16 x, flo
 template <> __device__ __forceinline__ __half scaled(__half x, float s) { return __float2half_rn(__half2float(x) * s); }
 
 // Elements c .. c + 7 of a row of codes, times scale, as bf16; those past the row's last block are zero.
-__device__ __forceinline__ uint4 mx_row8(const uint8_t* codes, const uint8_t* scales, int64_t kb, int64_t c, float scale)
+__device__ __forceinline__ uint4 mx_row8(const uint8_t* codes, const uint8_t* scales, uint32_t kb, uint32_t c, float scale)
 {
     const uint32_t* words = reinterpret_cast<const uint32_t*>(codes);
-    const int64_t i = c >> 3, b = c >> 5;
-    const uint32_t s = (uint32_t)c & 7u;
+    const uint32_t i = c >> 3, b = c >> 5, s = c & 7u;
     uint32_t w = __ldg(words + i);
-    if (s) w = __funnelshift_r(w, i + 1 < kb * 4 ? __ldg(words + i + 1) : 0u, 4u * s);
+    if (s) w = __funnelshift_r(w, i + 1u < kb * 4u ? __ldg(words + i + 1u) : 0u, 4u * s);
     const float f0 = mx_scale_value(__ldg(scales + b));
-    const uint32_t left = 32u - ((uint32_t)c & 31u);     // elements of this block from c on
-    const float f1 = left < 8u && b + 1 < kb ? mx_scale_value(__ldg(scales + b + 1)) : f0;
+    const uint32_t left = 32u - (c & 31u);               // elements of this block from c on
+    const float f1 = left < 8u && b + 1u < kb ? mx_scale_value(__ldg(scales + b + 1u)) : f0;
     float v[8];
     mx_expand8(w, v);
 #pragma unroll
@@ -83,66 +84,87 @@ __device__ __forceinline__ uint4 mx_row8(const uint8_t* codes, const uint8_t* sc
     return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
 
-template <typename T, bool kMx>
+// The same for c a multiple of 8: one word, one block.
+__device__ __forceinline__ uint4 mx_word8(uint32_t w, uint32_t e, float scale)
+{
+    const float f = mx_scale_value(e);
+    float v[8];
+    mx_expand8(w, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * f * scale;
+    return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+}
+
+// kEven: every output row starts on a 16-byte boundary
+template <typename T, bool kMx, bool kEven>
 __global__ void __launch_bounds__(kRowThreads)
 rows_kernel(Rows a)
 {
     constexpr int E = 16 / (int)sizeof(T);
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t base = (int64_t)blockIdx.x * (kRowThreads * kRowUnits), row_base = base / a.units;
-    const uint32_t rest = (uint32_t)(base - row_base * a.units);
-    const int64_t kb = mx_blocks(a.dim);
-    uint4 val[kRowUnits];
-    T* dst[kRowUnits];
-    int len[kRowUnits];
+    const uint32_t lanes = 1u << a.lanes_log2, in = threadIdx.x & (lanes - 1u);
+    const int64_t row = (((int64_t)blockIdx.x * kRowThreads) >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+    if (row >= a.n) return;
+    const int64_t src = a.tokens ? load_token(a.tokens, a.token_bytes, row) : row;
+    const bool known = src >= 0 && src < a.vocab;
+    if (!known && in == 0 && blockIdx.y == 0) atomicAdd(a.bad_index, 1ull);
+    T* out = reinterpret_cast<T*>(a.out) + row * a.ld;
+    const uint8_t* from = a.src + (known ? src : 0) * a.src_pitch;
+    const uint8_t* scales = a.scales + (known ? src : 0) * a.scale_pitch;
+    const uint32_t kb = (uint32_t)mx_blocks(a.dim), dim = (uint32_t)a.dim;
+    // elements ahead of the first boundary
+    const uint32_t head = kEven ? 0u : ((16u - ((uint32_t)reinterpret_cast<uintptr_t>(out) & 15u)) & 15u) / (uint32_t)sizeof(T);
+    for (uint32_t part = blockIdx.y; part < a.parts; part += gridDim.y) {
+        const uint32_t q0 = part * (lanes * kRowUnits) + in;
+        uint4 val[kRowUnits];
+        if constexpr (kMx && kEven) {                    // word and scale of every piece first
+            uint32_t w[kRowUnits], e[kRowUnits];
 #pragma unroll
-    for (int u = 0; u < kRowUnits; ++u) {
-        const uint32_t at = rest + threadIdx.x + u * kRowThreads;       // units < 2^28: no overflow
-        uint32_t r = __umulhi(at, a.magic), q = at - r * a.units;
-        if (q >= a.units) { q -= a.units; ++r; }
-        const int64_t row = row_base + r;
-        len[u] = 0;
-        val[u] = make_uint4(0u, 0u, 0u, 0u);
-        dst[u] = nullptr;
-        if (row >= a.n) continue;
-        T* out = reinterpret_cast<T*>(a.out) + row * a.ld;
-        const int head = (int)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(out) & 15u)) & 15u) / (int)sizeof(T);      // elements ahead of the first boundary
-        const int64_t c = head == 0 ? (int64_t)q * E : q == 0 ? 0 : head + (int64_t)(q - 1) * E;
-        if (c >= a.dim) continue;
-        len[u] = (int)min((int64_t)(head != 0 && q == 0 ? head : E), a.dim - c);
-        dst[u] = out + c;
-        const int64_t src = a.tokens ? load_token(a.tokens, a.token_bytes, row) : row;
-        if (src < 0 || src >= a.vocab) {
-            if (q == 0) atomicAdd(a.bad_index, 1ull);
-            continue;
-        }
-        const uint8_t* from = a.src + src * a.src_pitch;
-        if constexpr (kMx) {
-            val[u] = mx_row8(from, a.scales + src * a.scale_pitch, kb, c, a.scale);
-        } else {
-            const T* p = reinterpret_cast<const T*>(from) + c;
-            T* v = reinterpret_cast<T*>(&val[u]);
-            if (len[u] == E) val[u] = load16(reinterpret_cast<const uint8_t*>(p), a.src, a.src_end);
-            else {
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (j < len[u]) v[j] = p[j];
+            for (int u = 0; u < kRowUnits; ++u) {
+                const uint32_t q = q0 + u * lanes;
+                const bool there = known && q < a.units;
+                w[u] = there ? __ldg(reinterpret_cast<const uint32_t*>(from) + q) : 0u;
+                e[u] = there ? __ldg(scales + (q >> 2)) : 0u;
             }
-            if (a.scale != 1.0f) {
+#pragma unroll
+            for (int u = 0; u < kRowUnits; ++u) val[u] = mx_word8(w[u], e[u], a.scale);
+        }
+        uint32_t at[kRowUnits], len[kRowUnits];
+#pragma unroll
+        for (int u = 0; u < kRowUnits; ++u) {
+            const uint32_t q = q0 + u * lanes;
+            at[u] = head == 0u ? q * E : q == 0u ? 0u : head + (q - 1u) * E;
+            len[u] = q < a.units && at[u] < dim ? min(!kEven && head != 0u && q == 0u ? head : (uint32_t)E, dim - at[u]) : 0u;
+            if constexpr (!(kMx && kEven)) {
+                val[u] = make_uint4(0u, 0u, 0u, 0u);
+                if (len[u] == 0u || !known) continue;
+                if constexpr (kMx) val[u] = mx_row8(from, scales, kb, at[u], a.scale);
+                else {
+                    const T* p = reinterpret_cast<const T*>(from) + at[u];
+                    if (len[u] == (uint32_t)E) val[u] = load16(reinterpret_cast<const uint8_t*>(p), a.src, a.src_end);
+                    else {
+                        T* v = reinterpret_cast<T*>(&val[u]);
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+                            if (j < (int)len[u]) v[j] = p[j];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRowUnits; ++u) {
+            T* v = reinterpret_cast<T*>(&val[u]);
+            if (!kMx && a.scale != 1.0f) {
 #pragma unroll
                 for (int j = 0; j < E; ++j) v[j] = scaled(v[j], a.scale);
             }
-        }
-    }
+            if (len[u] == (uint32_t)E) *reinterpret_cast<uint4*>(out + at[u]) = val[u];
+            else {
 #pragma unroll
-    for (int u = 0; u < kRowUnits; ++u) {
-        if (len[u] == E) *reinterpret_cast<uint4*>(dst[u]) = val[u];
-        else {
-            const T* v = reinterpret_cast<const T*>(&val[u]);
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (j < len[u]) dst[u][j] = v[j];
+                for (int j = 0; j < E; ++j)
+                    if (j < (int)len[u]) out[at[u] + j] = v[j];
+            }
         }
     }
 }
@@ -153,20 +175,30 @@ int launch_rows(Rows a, cudaStream_t st)
     constexpr int E = 16 / (int)sizeof(T);
     const bool even = aligned(a.out, 16) && a.ld % E == 0;
     a.units = (uint32_t)((a.dim + E - 1) / E) + (even ? 0u : 1u);
-    a.magic = a.units == 1u ? 0xffffffffu : (uint32_t)((1ull << 32) / a.units);
-    const int64_t per_cta = kRowThreads * kRowUnits, ctas = (a.n * (int64_t)a.units + per_cta - 1) / per_cta;
-    if (ctas > 0x7fffffff) return LLVQ_EUNSUPPORTED;
-    return launch_pdl(rows_kernel<T, kMx>, (unsigned)ctas, kRowThreads, 0, st, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    a.lanes_log2 = 0;
+    while (a.lanes_log2 < 5 && (1u << a.lanes_log2) < a.units) ++a.lanes_log2;
+    const uint32_t per_part = kRowUnits << a.lanes_log2;
+    a.parts = (a.units + per_part - 1) / per_part;
+    const int64_t rows_per_cta = kRowThreads >> a.lanes_log2, ctas = (a.n + rows_per_cta - 1) / rows_per_cta;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas, std::min(a.parts, 65535u)); cfg.blockDim = dim3(kRowThreads); cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    const cudaError_t r = even ? cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, true>, a) : cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, false>, a);
+    return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 // ---- gradient -----------------------------------------------------------------------------------------------------------------------
 // grad[v] = scale * sum of dy[i] over the i with token v, in an order that the inputs alone fix: the positions are sorted by token
 // (stably), pieces of kPiece sorted positions are summed one position after the other in binary32, and the sums of a token whose positions
 // lie in several pieces are added in the order of the pieces.  No floating-point atomics.
-// Bound by HBM: dy is read and the gradient written once, and the rows that tokens name are written a second time, because all
-// rows are cleared while the sort is running: one cluster of eight thread blocks sorts, the others clear.
-constexpr int kSortCtas = 8, kSortWarps = 32, kSortBits = 9, kSortBins = 1 << kSortBits;
-constexpr int kPiece = 64;              // sorted positions per warp of the sums
+// Four kernels: one cluster of thread blocks sorts (a single block, without the cluster's barriers, up to 4096 tokens) while the next kernel
+// clears all rows; then the sums, then those of them that reach across pieces.
+// Bound by HBM: dy is read and the gradient written once, and the rows that tokens name are written a second time.
+constexpr int kSortWarps = 32, kSortBits = 9, kSortBins = 1 << kSortBits;
+constexpr int kClearBytes = 64 << 10;   // per thread block: many short ones write faster than a few that stay (2.1 GB: 300 us against 340)
 constexpr int kSpan = 256;              // columns per warp of the sums: eight per lane
 constexpr int kSumWarps = 8;
 
@@ -177,6 +209,7 @@ struct EmbedGrad {
     uint32_t *key[2], *pos[2];          // sorted from one into the other, digit by digit
     int passes, bits;                   // digits of `bits` bits
     int sorted;                         // which of the two is sorted at the end
+    int piece;                          // sorted positions per warp of the sums, at most 32
     const void* dy;
     void* grad;
     bool wide, accumulate;              // rows of dy and grad start on 16-byte boundaries; add to what grad holds
@@ -187,12 +220,13 @@ struct EmbedGrad {
 
 // One digit.  A warp takes a contiguous run of items, 32 at a time, in both loops; place of an item = items of smaller digits + of the same
 // digit in earlier thread blocks, warps and steps + in lower lanes.
+template <int kSortCtas>
 __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_t* total, uint32_t* base, uint32_t* warp_sum)
 {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << a.bits, shift = pass * a.bits;
-    const uint32_t rank = cluster.block_rank();
+    const uint32_t rank = kSortCtas > 1 ? cluster.block_rank() : 0u;
     const int64_t runs = kSortCtas * kSortWarps, run = (a.n + runs * 32 - 1) / (runs * 32) * 32;
     const int64_t begin = min((rank * kSortWarps + warp) * run, a.n), end = min(begin + run, a.n);
     const uint32_t *key = a.key[pass & 1], *pos = a.pos[pass & 1];
@@ -221,9 +255,10 @@ __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_
         for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = hist[w * kSortBins + tid]; hist[w * kSortBins + tid] = sum; sum += c; }
         total[tid] = sum;
     }
-    cluster.sync();
+    if (kSortCtas > 1) cluster.sync();
     uint32_t before = 0, all = 0;
-    if (tid < bins) {
+    if (kSortCtas == 1 && tid < bins) all = total[tid];
+    if (kSortCtas > 1 && tid < bins) {
         for (int c = 0; c < kSortCtas; ++c) {
             const uint32_t v = *cluster.map_shared_rank(total + tid, c);
             if (c < (int)rank) before += v;
@@ -257,32 +292,39 @@ __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_
             pos_out[at] = pass > 0 ? pos[i + lane] : (uint32_t)(i + lane);
         }
     }
-    cluster.sync();                                      // the next digit, and its counters, after all of this one; what was written is seen
+    if (kSortCtas > 1) cluster.sync();                   // the next digit, and its counters, after all of this one; what was written is seen
+    else __syncthreads();
 }
 
+template <int kSortCtas>
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortWarps * 32, 1)
-embed_sort_kernel(EmbedGrad a, uint8_t* clear, uint64_t clear_bytes)
+embed_sort_kernel(EmbedGrad a)
 {
     extern __shared__ __align__(16) uint32_t sort_smem[];
-    pdl_launch_dependents();
     pdl_wait();
-    if (blockIdx.x < kSortCtas) {
-        uint32_t* hist = sort_smem;
-        uint32_t *total = hist + kSortWarps * kSortBins, *base = total + kSortBins, *warp_sum = base + kSortBins;
-        for (int pass = 0; pass < a.passes; ++pass) sort_digit(a, pass, hist, total, base, warp_sum);
-        return;
+    pdl_launch_dependents();                             // behind the wait: the clearing kernel does not wait, and may write what an earlier kernel read
+    uint32_t* hist = sort_smem;
+    uint32_t *total = hist + kSortWarps * kSortBins, *base = total + kSortBins, *warp_sum = base + kSortBins;
+    for (int pass = 0; pass < a.passes; ++pass) sort_digit<kSortCtas>(a, pass, hist, total, base, warp_sum);
+}
+
+// Clears [p, p + bytes) while the sort is running.  Its last thread block ends after the sort has: what waits for this kernel finds both done.
+__global__ void __launch_bounds__(1024)
+embed_clear_kernel(uint8_t* p, uint64_t bytes)
+{
+    pdl_launch_dependents();
+    const uint64_t head = min((uint64_t)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(p) & 15u)) & 15u), bytes);      // up to the first 16-byte boundary
+    const uint64_t words = (bytes - head) / 16, tail = bytes - head - words * 16;
+    uint4* w = reinterpret_cast<uint4*>(p + head);
+    const uint64_t first = (uint64_t)blockIdx.x * (kClearBytes / 16) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kClearBytes / 16 / 1024; ++i)
+        if (first + i * 1024 < words) w[first + i * 1024] = make_uint4(0u, 0u, 0u, 0u);
+    if (blockIdx.x == 0) {
+        if (threadIdx.x < head) p[threadIdx.x] = 0;
+        if (threadIdx.x < tail) p[head + words * 16 + threadIdx.x] = 0;
     }
-    const uint32_t fillers = gridDim.x - kSortCtas, me = blockIdx.x - kSortCtas;
-    // clear [clear, clear + clear_bytes): bytes up to the first 16-byte boundary, 16 at a time, what is left
-    const uint64_t head = min((uint64_t)((16u - ((uint32_t)reinterpret_cast<uintptr_t>(clear) & 15u)) & 15u), clear_bytes);
-    const uint64_t words = (clear_bytes - head) / 16, tail = clear_bytes - head - words * 16;
-    uint4* w = reinterpret_cast<uint4*>(clear + head);
-    const uint64_t step = (uint64_t)fillers * blockDim.x;
-    for (uint64_t i = (uint64_t)me * blockDim.x + threadIdx.x; i < words; i += step) w[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (me == 0) {
-        if (threadIdx.x < head) clear[threadIdx.x] = 0;
-        if (threadIdx.x < tail) clear[head + words * 16 + threadIdx.x] = 0;
-    }
+    if (blockIdx.x == gridDim.x - 1) pdl_wait();
 }
 
 __device__ __forceinline__ float to_f(float x) { return x; }
@@ -350,7 +392,7 @@ __device__ __forceinline__ float* part_of(const EmbedGrad& a, int64_t piece, int
     return a.part + (piece * 2 + slot) * padded + col0 + lane * 8;
 }
 
-// A warp: kPiece sorted positions, kSpan columns.  Sums of tokens that begin and end inside the piece are final; the one that reaches in
+// A warp: a.piece sorted positions, kSpan columns.  Sums of tokens that begin and end inside the piece are final; the one that reaches in
 // from the piece before goes to slot 0 of the piece, the one that begins here and reaches into the next to slot 1.
 template <typename T, typename G, bool kWide>
 __global__ void __launch_bounds__(kSumWarps * 32)
@@ -359,22 +401,16 @@ embed_sum_kernel(EmbedGrad a, int64_t pieces, uint32_t spans)
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * kSumWarps + (threadIdx.x >> 5), piece = unit / spans;
+    const uint32_t unit = blockIdx.x * kSumWarps + (threadIdx.x >> 5), piece = unit / spans;
     if (piece >= pieces) return;
-    const int64_t col0 = (unit - piece * spans) * kSpan, first = piece * kPiece;
-    const int count = (int)min((int64_t)kPiece, a.n - first);
-    const uint32_t *keys = a.key[a.sorted], *poss = a.pos[a.sorted];
-    uint32_t key[kPiece / 32], pos[kPiece / 32];
-#pragma unroll
-    for (int h = 0; h < kPiece / 32; ++h) {
-        const bool in = h * 32 + lane < count;
-        key[h] = in ? keys[first + h * 32 + lane] : (uint32_t)a.vocab;
-        pos[h] = in ? poss[first + h * 32 + lane] : 0u;
-    }
-    const uint32_t key_before = first > 0 ? keys[first - 1] : (uint32_t)a.vocab;
-    const uint32_t key_after = first + count < a.n ? keys[first + count] : (uint32_t)a.vocab;
-    uint32_t cur = __shfl_sync(0xffffffffu, key[0], 0);
-    if (cur == (uint32_t)a.vocab) return;               // only what has no row is left
+    const int64_t col0 = (int64_t)(unit - piece * spans) * kSpan, first = (int64_t)piece * a.piece;
+    const int count = (int)min((int64_t)a.piece, a.n - first);
+    const uint32_t *keys = a.key[a.sorted], *poss = a.pos[a.sorted], none = (uint32_t)a.vocab;
+    const uint32_t key = lane < count ? keys[first + lane] : none, pos = lane < count ? poss[first + lane] : 0u;
+    const uint32_t key_before = first > 0 ? keys[first - 1] : none, key_after = first + count < a.n ? keys[first + count] : none;
+    const int used = __popc(__ballot_sync(0xffffffffu, key != none));      // what has no row sorts last
+    if (used == 0) return;
+    uint32_t cur = __shfl_sync(0xffffffffu, key, 0);
     bool from_before = cur == key_before;
     float sum[8] = {};
     auto flush = [&](bool goes_on) {
@@ -390,32 +426,27 @@ embed_sum_kernel(EmbedGrad a, int64_t pieces, uint32_t spans)
         for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
     };
     constexpr int kAhead = sizeof(T) == 4 ? 4 : 8;       // rows in flight
-    bool over = false;
+    for (int i0 = 0; i0 < used; i0 += kAhead) {
+        Span<T, kWide> s[kAhead];
 #pragma unroll
-    for (int h = 0; h < kPiece / 32; ++h) {
-        for (int i0 = 0; i0 < 32 && !over; i0 += kAhead) {
-            Span<T, kWide> s[kAhead];
-            uint32_t k[kAhead];
+        for (int i = 0; i < kAhead; ++i) {
+            const uint32_t p = __shfl_sync(0xffffffffu, pos, (i0 + i) & 31);
+            if (i0 + i < used) load_span<T, kWide>(s[i], static_cast<const T*>(a.dy) + (int64_t)p * a.dim, col0, lane, a.dim);
+        }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                k[i] = __shfl_sync(0xffffffffu, key[h], i0 + i);
-                const uint32_t p = __shfl_sync(0xffffffffu, pos[h], i0 + i);
-                if (k[i] != (uint32_t)a.vocab) load_span<T, kWide>(s[i], static_cast<const T*>(a.dy) + (int64_t)p * a.dim, col0, lane, a.dim);
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (over) break;
-                if (k[i] != cur) {
+        for (int i = 0; i < kAhead; ++i) {
+            if (i0 + i < used) {
+                const uint32_t k = __shfl_sync(0xffffffffu, key, (i0 + i) & 31);
+                if (k != cur) {
                     flush(false);
-                    cur = k[i];
-                    if (cur == (uint32_t)a.vocab) { over = true; break; }
+                    cur = k;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] += to_f(s[i].v[j]);
             }
         }
     }
-    if (!over) flush(cur == key_after);
+    flush(cur == key_after);
 }
 
 // Sums that reach across pieces: a thread block takes those that begin in its piece (there is one at most), for kSpan columns, and its
@@ -428,16 +459,16 @@ embed_join_kernel(EmbedGrad a, int64_t pieces, uint32_t spans)
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t piece = blockIdx.x / spans, col0 = (int64_t)(blockIdx.x % spans) * kSpan, last = (piece + 1) * kPiece - 1;
+    const int64_t piece = blockIdx.x / spans, col0 = (int64_t)(blockIdx.x % spans) * kSpan, last = (piece + 1) * a.piece - 1;
     const uint32_t* keys = a.key[a.sorted];
     if (last + 1 >= a.n) return;
     const uint32_t key = keys[last];
     if (key == (uint32_t)a.vocab || keys[last + 1] != key) return;                        // nothing reaches out of the piece
-    if (piece > 0 && keys[piece * kPiece] == key && keys[piece * kPiece - 1] == key) return;   // it began in an earlier one
+    if (piece > 0 && keys[piece * a.piece] == key && keys[piece * a.piece - 1] == key) return;   // it began in an earlier one
     int64_t lo = piece + 1, hi = pieces;                // first piece that does not begin with the token
     while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
-        if (keys[mid * kPiece] == key) lo = mid + 1;
+        if (keys[mid * a.piece] == key) lo = mid + 1;
         else hi = mid;
     }
     const int64_t more = lo - (piece + 1), run = (more + kSumWarps - 1) / kSumWarps;
@@ -471,13 +502,20 @@ int bits_of(uint64_t v)
     return b;
 }
 
+// Positions per warp of the sums: as many as leave a warp to every slot of 148 SMs with 24 each, 32 at most and 8 at least.
+int piece_of(int64_t n, int64_t dim)
+{
+    int piece = 32;
+    while (piece > 8 && (n + piece - 1) / piece * ((dim + kSpan - 1) / kSpan) < 148 * 24) piece /= 2;
+    return piece;
+}
+
 uint64_t round256(uint64_t v) { return (v + 255) / 256 * 256; }
 
 template <typename T, typename G, bool kWide>
 int launch_sums(const EmbedGrad& a, int64_t pieces, uint32_t spans, cudaStream_t st)
 {
     const int64_t ctas = (pieces * (int64_t)spans + kSumWarps - 1) / kSumWarps;
-    if (pieces * (int64_t)spans > 0x7fffffff) return LLVQ_EUNSUPPORTED;
     if (launch_pdl(embed_sum_kernel<T, G, kWide>, (unsigned)ctas, kSumWarps * 32, 0, st, a, pieces, spans) != cudaSuccess) return LLVQ_ECUDA;
     if (pieces > 1 && launch_pdl(embed_join_kernel<G, kWide>, (unsigned)(pieces * spans), kSumWarps * 32, 0, st, a, pieces, spans) != cudaSuccess) return LLVQ_ECUDA;
     return launch_status();
@@ -510,7 +548,7 @@ int llvq_mx_dequant_matrix(const llvq_ctx* ctx, const uint8_t* d_codes, const ui
     if (ctx && ctx->device >= 0 && (rows == 0 || cols == 0)) return LLVQ_OK;      // nothing to do: pointers may be null
     if (!ctx || ctx->device < 0 || !d_codes || !d_scales || !d_w_bf16 || rows < 0 || cols < 0 || ld < cols) return LLVQ_EINVAL;
     if (!aligned(d_codes, 16) || !aligned(d_scales, 16) || !aligned(d_w_bf16, 2)) return LLVQ_EALIGN;
-    if (rows > (1ll << 31) || cols > (1ll << 31)) return LLVQ_EUNSUPPORTED;
+    if (rows > 0x7fffffffll || cols > (1ll << 30)) return LLVQ_EUNSUPPORTED;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return LLVQ_ECUDA;
     Rows a{};
@@ -527,7 +565,7 @@ int llvq_embed(const llvq_ctx* ctx, const void* d_table, int dtype, int64_t voca
     if (!dtype_ok(dtype) || (token_bytes != 4 && token_bytes != 8)) return LLVQ_EINVAL;
     const int es = size_of(dtype);
     if (!aligned(d_table, es) || !aligned(d_out, es) || !aligned(d_tokens, token_bytes)) return LLVQ_EALIGN;
-    if (vocab > (1ll << 31) || dim > (1ll << 31) || n > (1ll << 31)) return LLVQ_EUNSUPPORTED;
+    if (vocab > 0x7fffffffll || dim > (1ll << 30) || n > 0x7fffffffll) return LLVQ_EUNSUPPORTED;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return LLVQ_ECUDA;
     Rows a{};
@@ -545,7 +583,7 @@ int llvq_mx_embed(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_
     if (!ctx || ctx->device < 0 || !d_codes || !d_scales || !d_tokens || !d_out_bf16 || vocab <= 0 || dim < 0 || n < 0) return LLVQ_EINVAL;
     if (token_bytes != 4 && token_bytes != 8) return LLVQ_EINVAL;
     if (!aligned(d_codes, 16) || !aligned(d_scales, 16) || !aligned(d_out_bf16, 2) || !aligned(d_tokens, token_bytes)) return LLVQ_EALIGN;
-    if (vocab > (1ll << 31) || dim > (1ll << 31) || n > (1ll << 31)) return LLVQ_EUNSUPPORTED;
+    if (vocab > 0x7fffffffll || dim > (1ll << 30) || n > 0x7fffffffll) return LLVQ_EUNSUPPORTED;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return LLVQ_ECUDA;
     Rows a{};
@@ -558,7 +596,7 @@ int llvq_mx_embed(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_
 size_t llvq_embed_grad_bytes(int64_t n, int64_t dim)
 {
     if (n <= 0 || dim <= 0 || n >= (1ll << 31) || dim > (1ll << 31)) return 0;
-    const uint64_t pieces = ((uint64_t)n + kPiece - 1) / kPiece, padded = ((uint64_t)dim + kSpan - 1) / kSpan * kSpan;
+    const uint64_t piece = (uint64_t)piece_of(n, dim), pieces = ((uint64_t)n + piece - 1) / piece, padded = ((uint64_t)dim + kSpan - 1) / kSpan * kSpan;
     const unsigned __int128 all = (unsigned __int128)4 * round256((uint64_t)n * 4) + (unsigned __int128)pieces * 2 * padded * 4;
     return all > ((unsigned __int128)1 << 62) ? 0 : (size_t)all;
 }
@@ -592,15 +630,16 @@ int llvq_embed_grad(const llvq_ctx* ctx, const void* d_dy, int dy_dtype, const v
     a.sorted = a.passes & 1;
     a.dy = d_dy; a.grad = d_grad; a.accumulate = accumulate != 0; a.scale = scale; a.bad_index = ctx->dev.bad_index;
     a.wide = aligned(d_dy, 16) && aligned(d_grad, 16) && dim * es % 16 == 0 && dim * gs % 16 == 0;
-    const uint64_t clear = accumulate ? 0 : (uint64_t)vocab * (uint64_t)dim * gs;
-    const size_t smem = (size_t)(kSortWarps * kSortBins + 2 * kSortBins + kSortWarps) * 4;
-    if (!set_smem<embed_sort_kernel>(ctx, smem)) return LLVQ_ECUDA;
-    // thread blocks that clear: 256 KB each at least, two per SM at most
-    const uint64_t wanted = (clear + (256u << 10) - 1) / (256u << 10), most = (uint64_t)ctx->sm_count * 2 / kSortCtas * kSortCtas;
-    const unsigned clearing = (unsigned)(std::min(wanted, most) + kSortCtas - 1) / kSortCtas * kSortCtas;
-    if (launch_pdl(embed_sort_kernel, kSortCtas + clearing, kSortWarps * 32, smem, st, a, static_cast<uint8_t*>(d_grad), clear) != cudaSuccess) return LLVQ_ECUDA;
-    const int64_t pieces = (n + kPiece - 1) / kPiece;
+    a.piece = piece_of(n, dim);
+    const uint64_t clear = accumulate ? 0 : (uint64_t)vocab * (uint64_t)dim * gs, clearing = (clear + 15 + kClearBytes - 1) / kClearBytes;
+    const int64_t pieces = (n + a.piece - 1) / a.piece;
     const uint32_t spans = (uint32_t)((dim + kSpan - 1) / kSpan);
+    if (clearing > 0x7fffffff || pieces * (int64_t)spans > 0x7fffffff) return LLVQ_EUNSUPPORTED;
+    const size_t smem = (size_t)(kSortWarps * kSortBins + 2 * kSortBins + kSortWarps) * 4;
+    if (!set_smem<embed_sort_kernel<1>>(ctx, smem) || !set_smem<embed_sort_kernel<8>>(ctx, smem)) return LLVQ_ECUDA;
+    const cudaError_t r = n <= 4096 ? launch_pdl(embed_sort_kernel<1>, 1u, kSortWarps * 32, smem, st, a) : launch_pdl(embed_sort_kernel<8>, 8u, kSortWarps * 32, smem, st, a);
+    if (r != cudaSuccess) return LLVQ_ECUDA;
+    if (!accumulate && launch_pdl(embed_clear_kernel, (unsigned)clearing, 1024, 0, st, static_cast<uint8_t*>(d_grad), clear) != cudaSuccess) return LLVQ_ECUDA;
     return dy_dtype == LLVQ_F32    ? launch_sums<float>(a, grad_dtype, pieces, spans, st)
            : dy_dtype == LLVQ_BF16 ? launch_sums<__nv_bfloat16>(a, grad_dtype, pieces, spans, st)
                                    : launch_sums<__half>(a, grad_dtype, pieces, spans, st);

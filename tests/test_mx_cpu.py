@@ -31,8 +31,9 @@ def test_pitches(P, cols):
 def test_workspace_of_the_gradient(P):
     L = P.load_library()
     assert L.llvq_embed_grad_bytes(0, 8) == 0 and L.llvq_embed_grad_bytes(8, 0) == 0 and L.llvq_embed_grad_bytes(1 << 31, 8) == 0
-    for n, dim in ((1, 1), (64, 512), (65, 513), (100000, 4096)):
-        lists, pieces, padded = 4 * (-(-n * 4 // 256) * 256), -(-n // 64), -(-dim // 256) * 256
+    # lists of keys and positions, twice; two sums per piece of 8 positions at the smallest, 32 at the largest, for columns rounded up to 256
+    for n, dim, piece in ((1, 1, 8), (64, 512, 8), (65, 513, 8), (100000, 4096, 32)):
+        lists, pieces, padded = 4 * (-(-n * 4 // 256) * 256), -(-n // piece), -(-dim // 256) * 256
         assert L.llvq_embed_grad_bytes(n, dim) == lists + pieces * 2 * padded * 4
 
 
