@@ -84,19 +84,29 @@ __device__ __forceinline__ uint4 mx_row8(const uint8_t* codes, const uint8_t* sc
     return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
 
+// Two products with one factor.
+__device__ __forceinline__ void scale_pair(float& x, float& y, float f)
+{
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%0, %1};\n mov.b64 b, {%2, %2};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}" : "+f"(x), "+f"(y) : "f"(f));
+}
+
 // The same for c a multiple of 8: one word, one block.
-__device__ __forceinline__ uint4 mx_word8(uint32_t w, uint32_t e, float scale)
+__device__ __forceinline__ uint4 mx_word8(uint32_t w, uint32_t e, float scale, bool times)
 {
     const float f = mx_scale_value(e);
     float v[8];
     mx_expand8(w, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * f * scale;
+    for (int j = 0; j < 8; j += 2) scale_pair(v[j], v[j + 1], f);
+    if (times) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) scale_pair(v[j], v[j + 1], scale);
+    }
     return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
 
-// kEven: every output row starts on a 16-byte boundary
-template <typename T, bool kMx, bool kEven>
+// kEven: every output row starts on a 16-byte boundary.  kWhole: and is a whole number of pieces, as is every row of the table
+template <typename T, bool kMx, bool kEven, bool kWhole>
 __global__ void __launch_bounds__(kRowThreads)
 rows_kernel(Rows a)
 {
@@ -118,52 +128,81 @@ rows_kernel(Rows a)
     for (uint32_t part = blockIdx.y; part < a.parts; part += gridDim.y) {
         const uint32_t q0 = part * (lanes * kRowUnits) + in;
         uint4 val[kRowUnits];
-        if constexpr (kMx && kEven) {                    // word and scale of every piece first
-            uint32_t w[kRowUnits], e[kRowUnits];
+        if constexpr (kWhole) {
+            const bool times = a.scale != 1.0f;
+            if (kMx) {
+                uint32_t w[kRowUnits], e[kRowUnits];
 #pragma unroll
-            for (int u = 0; u < kRowUnits; ++u) {
-                const uint32_t q = q0 + u * lanes;
-                const bool there = known && q < a.units;
-                w[u] = there ? __ldg(reinterpret_cast<const uint32_t*>(from) + q) : 0u;
-                e[u] = there ? __ldg(scales + (q >> 2)) : 0u;
-            }
+                for (int u = 0; u < kRowUnits; ++u) {
+                    const uint32_t q = min(q0 + u * lanes, a.units - 1u);
+                    w[u] = __ldg(reinterpret_cast<const uint32_t*>(from) + q);
+                    e[u] = __ldg(scales + (q >> 2));
+                }
 #pragma unroll
-            for (int u = 0; u < kRowUnits; ++u) val[u] = mx_word8(w[u], e[u], a.scale);
-        }
-        uint32_t at[kRowUnits], len[kRowUnits];
+                for (int u = 0; u < kRowUnits; ++u) val[u] = mx_word8(w[u], e[u], a.scale, times);
+            } else {
 #pragma unroll
-        for (int u = 0; u < kRowUnits; ++u) {
-            const uint32_t q = q0 + u * lanes;
-            at[u] = head == 0u ? q * E : q == 0u ? 0u : head + (q - 1u) * E;
-            len[u] = q < a.units && at[u] < dim ? min(!kEven && head != 0u && q == 0u ? head : (uint32_t)E, dim - at[u]) : 0u;
-            if constexpr (!(kMx && kEven)) {
-                val[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (len[u] == 0u || !known) continue;
-                if constexpr (kMx) val[u] = mx_row8(from, scales, kb, at[u], a.scale);
-                else {
-                    const T* p = reinterpret_cast<const T*>(from) + at[u];
-                    if (len[u] == (uint32_t)E) val[u] = load16(reinterpret_cast<const uint8_t*>(p), a.src, a.src_end);
-                    else {
+                for (int u = 0; u < kRowUnits; ++u) val[u] = __ldg(reinterpret_cast<const uint4*>(from) + min(q0 + u * lanes, a.units - 1u));
+                if (times) {
+#pragma unroll
+                    for (int u = 0; u < kRowUnits; ++u) {
                         T* v = reinterpret_cast<T*>(&val[u]);
 #pragma unroll
-                        for (int j = 0; j < E; ++j)
-                            if (j < (int)len[u]) v[j] = p[j];
+                        for (int j = 0; j < E; ++j) v[j] = scaled(v[j], a.scale);
                     }
                 }
             }
-        }
 #pragma unroll
-        for (int u = 0; u < kRowUnits; ++u) {
-            T* v = reinterpret_cast<T*>(&val[u]);
-            if (!kMx && a.scale != 1.0f) {
+            for (int u = 0; u < kRowUnits; ++u)
+                if (q0 + u * lanes < a.units) reinterpret_cast<uint4*>(out)[q0 + u * lanes] = known ? val[u] : make_uint4(0u, 0u, 0u, 0u);
+        } else {
+            if constexpr (kMx && kEven) {                    // word and scale of every piece first
+                uint32_t w[kRowUnits], e[kRowUnits];
 #pragma unroll
-                for (int j = 0; j < E; ++j) v[j] = scaled(v[j], a.scale);
+                for (int u = 0; u < kRowUnits; ++u) {
+                    const uint32_t q = q0 + u * lanes;
+                    const bool there = known && q < a.units;
+                    w[u] = there ? __ldg(reinterpret_cast<const uint32_t*>(from) + q) : 0u;
+                    e[u] = there ? __ldg(scales + (q >> 2)) : 0u;
+                }
+#pragma unroll
+                for (int u = 0; u < kRowUnits; ++u) val[u] = mx_word8(w[u], e[u], a.scale, true);
             }
-            if (len[u] == (uint32_t)E) *reinterpret_cast<uint4*>(out + at[u]) = val[u];
-            else {
+            uint32_t at[kRowUnits], len[kRowUnits];
 #pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (j < (int)len[u]) out[at[u] + j] = v[j];
+            for (int u = 0; u < kRowUnits; ++u) {
+                const uint32_t q = q0 + u * lanes;
+                at[u] = head == 0u ? q * E : q == 0u ? 0u : head + (q - 1u) * E;
+                len[u] = q < a.units && at[u] < dim ? min(!kEven && head != 0u && q == 0u ? head : (uint32_t)E, dim - at[u]) : 0u;
+                if constexpr (!(kMx && kEven)) {
+                    val[u] = make_uint4(0u, 0u, 0u, 0u);
+                    if (len[u] == 0u || !known) continue;
+                    if constexpr (kMx) val[u] = mx_row8(from, scales, kb, at[u], a.scale);
+                    else {
+                        const T* p = reinterpret_cast<const T*>(from) + at[u];
+                        if (len[u] == (uint32_t)E) val[u] = load16(reinterpret_cast<const uint8_t*>(p), a.src, a.src_end);
+                        else {
+                            T* v = reinterpret_cast<T*>(&val[u]);
+#pragma unroll
+                            for (int j = 0; j < E; ++j)
+                                if (j < (int)len[u]) v[j] = p[j];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kRowUnits; ++u) {
+                T* v = reinterpret_cast<T*>(&val[u]);
+                if (!kMx && a.scale != 1.0f) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[j] = scaled(v[j], a.scale);
+                }
+                if (len[u] == (uint32_t)E) *reinterpret_cast<uint4*>(out + at[u]) = val[u];
+                else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+                        if (j < (int)len[u]) out[at[u] + j] = v[j];
+                }
             }
         }
     }
@@ -186,7 +225,10 @@ int launch_rows(Rows a, cudaStream_t st)
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
-    const cudaError_t r = even ? cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, true>, a) : cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, false>, a);
+    const bool whole = even && a.dim % E == 0 && (kMx || aligned(a.src, 16));
+    const cudaError_t r = whole  ? cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, true, true>, a)
+                          : even ? cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, true, false>, a)
+                                 : cudaLaunchKernelEx(&cfg, rows_kernel<T, kMx, false, false>, a);
     return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 

@@ -13,10 +13,9 @@ using namespace llvq;
 constexpr int kMxThreads = 256;
 
 // ---- quantisation ---------------------------------------------------------------------------------------------------------------
-// Four lanes per block of 32, eight elements each; the largest exponent of the block is the exponent of its largest magnitude, found
-// on the bit patterns.  scale = 2^(exponent - 2): the largest element lands in [4, 8), what is above 6 becomes 6.  A warp takes eight
-// blocks of a row at a time (their eight scale bytes are one store) and kMxUnroll such pieces together, so that its loads overlap.
-// Bound by HBM: the input is read once and a quarter (bf16) of its bytes written.
+// Four lanes per block of 32, eight elements each.  scale = 2^(exponent of the largest magnitude - 2): the largest element lands in [4, 8), what is
+// above 6 becomes 6.  A warp takes kMxUnroll pieces of eight blocks of one row, so that its loads overlap and its addresses are worked
+// out once.  Bound by HBM: the input is read once and a quarter (bf16) or an eighth (binary32) of its bytes written.
 constexpr int kMxUnroll = 4;
 
 template <typename T> struct Wide;      // eight elements as they are loaded
@@ -47,62 +46,64 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 
+// The larger of m and |v|; NaN if either is.
+__device__ __forceinline__ float max_abs(float m, float v)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(v)));
+    return r;
+}
+
 // wide: rows start on 16-byte boundaries
 template <typename T>
 __global__ void __launch_bounds__(kMxThreads)
-mx_quantize_kernel(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld, uint32_t pieces, bool wide, uint8_t* __restrict__ codes,
+mx_quantize_kernel(const T* __restrict__ x, int64_t rows, uint32_t cols, int64_t ld, uint32_t kb, uint32_t pitch, bool wide, uint8_t* __restrict__ codes,
                    uint8_t* __restrict__ scales)
 {
     pdl_launch_dependents();
     pdl_wait();
-    const uint32_t lane = threadIdx.x & 31u;
-    const int64_t kb = mx_blocks(cols), total = rows * (int64_t)pieces;
-    const int64_t first = ((int64_t)blockIdx.x * (kMxThreads / 32) + (threadIdx.x >> 5)) * kMxUnroll;
-    int64_t row = first / pieces;
-    uint32_t piece = (uint32_t)(first - row * pieces);
-    float v[kMxUnroll][8];
-    int64_t at_row[kMxUnroll];
-    uint32_t at_piece[kMxUnroll];
+    const uint32_t lane = threadIdx.x & 31u, parts = (pitch + 8u * kMxUnroll - 1u) / (8u * kMxUnroll);
+    const int64_t row = (int64_t)blockIdx.x * (kMxThreads / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const T* from = x + row * ld;
+    uint8_t *codes_row = codes + row * (int64_t)(kb * kMxBlockBytes), *scales_row = scales + row * (int64_t)pitch;
+    for (uint32_t part = blockIdx.y; part < parts; part += gridDim.y) {
+        const uint32_t c0 = part * (256u * kMxUnroll) + lane * 8u, b0 = c0 >> 5;
+        float v[kMxUnroll][8];
+        if (wide && (part + 1u) * (256u * kMxUnroll) <= cols) {
+            Wide<T> w[kMxUnroll];
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
-        at_row[u] = first + u < total ? row : -1;
-        at_piece[u] = piece;
-        if (++piece == pieces) { piece = 0; ++row; }
-        const int64_t c = (int64_t)at_piece[u] * 256 + lane * 8;
-        const T* p = x + at_row[u] * ld + c;
-        if (at_row[u] >= 0 && wide && c + 8 <= cols) {
-            widen(*reinterpret_cast<const Wide<T>*>(p), v[u]);
+            for (int u = 0; u < kMxUnroll; ++u) w[u] = *reinterpret_cast<const Wide<T>*>(from + c0 + u * 256);
+#pragma unroll
+            for (int u = 0; u < kMxUnroll; ++u) widen(w[u], v[u]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[u][j] = at_row[u] >= 0 && c + j < cols ? to_float(p[j]) : 0.0f;
+            for (int u = 0; u < kMxUnroll; ++u) {
+                const uint32_t c = c0 + u * 256;
+                if (wide && c + 8u <= cols) widen(*reinterpret_cast<const Wide<T>*>(from + c), v[u]);
+                else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[u][j] = c + j < cols ? to_float(from[c + j]) : 0.0f;
+                }
+            }
         }
-    }
 #pragma unroll
-    for (int u = 0; u < kMxUnroll; ++u) {
-        if (at_row[u] < 0) break;                       // the same for the whole warp
-        uint32_t most = 0;
+        for (int u = 0; u < kMxUnroll; ++u) {
+            float most = fabsf(v[u][0]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(v[u][j]) & 0x7fffffffu);
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
-        most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        const int exponent = (int)(most >> 23);         // 255: an infinity or a NaN among them
-        const uint32_t e = exponent == 255 ? 255u : (uint32_t)max(exponent - 2, 0);
-        const float unit = e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);       // 2^(127 - e): e is at most 252, a multiplication that is exact
-        uint32_t w = 0;                                                              // unless the product is far below the smallest element
-        if (e != 255u) {
-            float q[8];
+            for (int j = 1; j < 8; ++j) most = max_abs(most, v[u][j]);
+            most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = max_abs(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const uint32_t exponent = __float_as_uint(most) >> 23;         // 255: an infinity or a NaN among them
+            const uint32_t e = exponent == 255u ? 255u : max(exponent, 2u) - 2u;
+            const float unit = __uint_as_float((254u - min(e, 252u)) << 23);      // 2^(127 - e) (255: not used); the product is exact unless it is
+            float q[8];                                                         // far below the smallest element
 #pragma unroll
             for (int j = 0; j < 8; ++j) q[j] = v[u][j] * unit;
-            w = mx_pack8(q);
+            const uint32_t w = e == 255u ? 0u : mx_pack8(q), b = b0 + u * 8u;
+            if (b < kb) *reinterpret_cast<uint32_t*>(codes_row + (c0 + u * 256u) / 2u) = w;
+            if ((lane & 3u) == 0u && b < pitch) scales_row[b] = b < kb ? (uint8_t)e : (uint8_t)0;
         }
-        const int64_t block = (int64_t)at_piece[u] * 8 + (lane >> 2);
-        if (block < kb) *reinterpret_cast<uint32_t*>(codes + at_row[u] * (kb * kMxBlockBytes) + block * kMxBlockBytes + (lane & 3u) * 4) = w;
-        // the eight scale bytes, those past the row's end zero, by the first lane
-        uint32_t byte = block < kb ? e : 0u;
-        byte |= __shfl_down_sync(0xffffffffu, byte, 4) << 8;
-        byte |= __shfl_down_sync(0xffffffffu, byte, 8) << 16;
-        const uint32_t above = __shfl_down_sync(0xffffffffu, byte, 16);
-        if (lane == 0) *reinterpret_cast<uint2*>(scales + at_row[u] * (int64_t)pieces * 8 + at_piece[u] * 8) = make_uint2(byte, above);
     }
 }
 
@@ -471,7 +472,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
 }
 
 // Sizes whose byte counts leave 63 bits, or dimensions that the kernels' indices do not hold.
-bool mx_too_large(int64_t rows, int64_t cols) { return rows > (1ll << 31) || cols > (1ll << 31); }
+bool mx_too_large(int64_t rows, int64_t cols) { return rows > 0x7fffffffll || cols > (1ll << 30); }
 
 // none: the matrix has no columns, and its arrays may be null
 int mx_check(const llvq_ctx* ctx, bool none, const uint8_t* d_codes, const uint8_t* d_scales)
@@ -484,10 +485,14 @@ template <typename T>
 cudaError_t launch_quantize(const void* x, int64_t rows, int64_t cols, int64_t ld, uint8_t* codes, uint8_t* scales, cudaStream_t st)
 {
     const bool wide = aligned(x, 16) && ld % (16 / (int64_t)sizeof(T)) == 0;
-    const uint32_t pieces = (uint32_t)(mx_scale_pitch(cols) / 8);
-    const int64_t per_cta = kMxThreads / 32 * kMxUnroll, ctas = (rows * (int64_t)pieces + per_cta - 1) / per_cta;
-    if (ctas > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_pdl(mx_quantize_kernel<T>, (unsigned)ctas, kMxThreads, 0, st, static_cast<const T*>(x), rows, cols, ld, pieces, wide, codes, scales);
+    const uint32_t pitch = (uint32_t)mx_scale_pitch(cols), parts = (pitch + 8u * kMxUnroll - 1u) / (8u * kMxUnroll);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((rows + kMxThreads / 32 - 1) / (kMxThreads / 32)), std::min(parts, 65535u)); cfg.blockDim = dim3(kMxThreads); cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mx_quantize_kernel<T>, static_cast<const T*>(x), rows, (uint32_t)cols, ld, (uint32_t)mx_blocks(cols), pitch, wide, codes, scales);
 }
 
 template <int kWarps, int kTiles, bool kF32, bool kPre>
@@ -568,7 +573,7 @@ int llvq_mx_quantize(const llvq_ctx* ctx, const void* d_x, int x_dtype, int64_t 
     const cudaError_t r = x_dtype == LLVQ_F32    ? launch_quantize<float>(d_x, rows, cols, ld, d_codes, d_scales, st)
                           : x_dtype == LLVQ_BF16 ? launch_quantize<__nv_bfloat16>(d_x, rows, cols, ld, d_codes, d_scales, st)
                                                  : launch_quantize<__half>(d_x, rows, cols, ld, d_codes, d_scales, st);
-    return r == cudaSuccess ? launch_status() : r == cudaErrorInvalidValue ? LLVQ_EUNSUPPORTED : LLVQ_ECUDA;
+    return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x_bf16, void* d_y,
