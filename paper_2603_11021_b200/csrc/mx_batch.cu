@@ -26,6 +26,7 @@ using namespace llvq;
 // Bound by HBM for few rows of X; at 64 the products take as long as the reads.
 constexpr int kBatchRows = 128, kBatchCols = 128, kBatchThreads = 352;
 constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a stage's weights, a byte of room per element
+constexpr int kRawScales = 4;                             // boxes of scales under way: 128 rows, 16 blocks, for four steps each
 
 __host__ __device__ inline uint32_t batch_npad(int batch) { return (3u * (uint32_t)batch + 15u) / 16u * 16u; }
 __host__ __device__ inline uint32_t batch_x_bytes(uint32_t npad) { return npad * 128u + 2u * kScaleAtom; }      // of a chunk
@@ -173,32 +174,35 @@ __device__ __noinline__ float dot_plain(const BatchArgs& a, int64_t row, int n)
     return sum;
 }
 
-__device__ __forceinline__ void put_y(const BatchArgs& a, int64_t row, int n, float v)
+__device__ __forceinline__ void put_y(const BatchArgs& a, int64_t row, int n, float v) { a.y[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(v); }
+
+// Where a result is NaN: rows of X with an infinity (and no NaN) once more.
+__device__ __noinline__ void mend_row(const BatchArgs& a, int64_t row)
 {
-    if (row >= a.n_out) return;
-    if (v != v) {                                         // NaN stays where X has one; else an infinity may be behind it
+    for (int n = 0; n < a.batch; ++n) {
         bool nan = false, inf = false;
         for (uint32_t c = 0; c < a.steps; ++c) { const uint8_t note = a.notes[(uint64_t)c * a.batch + n]; nan |= note == 2; inf |= note == 1; }
-        if (inf && !nan) v = dot_plain(a, row, n);
+        if (inf && !nan) put_y(a, row, n, dot_plain(a, row, n));
     }
-    a.y[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(v);
 }
 
 template <int kStages>
 __global__ void __launch_bounds__(kBatchThreads, 1)
-mx_batch_kernel(BatchArgs a)
+mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
 {
+    constexpr int kLag = (kStages + 1) / 2;               // copies of codes are announced when kLag later ones are under way: the other stages keep the MMAs fed
     extern __shared__ uint8_t mb_smem[];
-    __shared__ uint64_t full[kStages], empty[kStages], acc_full, acc_empty;
+    __shared__ uint64_t full[kStages], empty[kStages], raw_full[kRawScales], acc_full, acc_empty;
     __shared__ uint32_t tmem_slot, last_slot;
     const uint32_t base = (smem_u32(mb_smem) + 1023u) & ~1023u;
     const uint32_t x_bytes = batch_x_bytes(a.npad), stage_bytes = (kBatchA + x_bytes + kScaleAtom + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
     const uint64_t units = (uint64_t)a.tiles * a.steps, begin = share_begin(units, gridDim.x, blockIdx.x), end = share_begin(units, gridDim.x, blockIdx.x + 1);
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full + s, 128 + 2); mbar_init(empty + s, 1); }       // 128 threads' copies of codes, scales, X
+        for (int s = 0; s < kStages; ++s) { mbar_init(full + s, 4 + 2); mbar_init(empty + s, 1); }       // four warps' copies of codes, scales, X
+        for (int e = 0; e < kRawScales; ++e) mbar_init(raw_full + e, 1);
         mbar_init(&acc_full, 1);
         mbar_init(&acc_empty, 4);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -211,40 +215,75 @@ mx_batch_kernel(BatchArgs a)
     bool ok = true;
     uint32_t s = 0, phase = 0;
     auto next = [&] { if (++s == (uint32_t)kStages) { s = 0; phase ^= 1u; } };
-    uint32_t it = 0;                                      // stages so far
+    const uint32_t total = (uint32_t)(end - begin);
+    uint32_t tile = (uint32_t)(begin / a.steps), step = (uint32_t)(begin - (uint64_t)tile * a.steps), it = 0;      // it: stages so far
+    auto advance = [&] { ++it; next(); if (++step == a.steps) { step = 0; ++tile; } };
 
     if (warp >= 4 && warp < 8) {
         const uint32_t p = threadIdx.x - 128u, c = p & 7u, r = p >> 3;          // container of a row; rows r, r + 16, ...
         const uint32_t to = base + r * 128u + ((c ^ (r & 7u)) << 4);
-        for (uint64_t u = begin; u < end && ok; ++u, ++it) {
-            const uint32_t tile = (uint32_t)(u / a.steps), step = (uint32_t)(u - (uint64_t)tile * a.steps);
+        uint32_t announced = 0, at = 0;
+        auto announce = [&] {                             // what this warp has copied for the next stage becomes visible to the tensor cores
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive(full + at);
+            ++announced;
+            if (++at == (uint32_t)kStages) at = 0;
+        };
+        const uint8_t* from = a.codes + ((int64_t)tile * kBatchRows + r) * a.code_pitch + c * 8u;      // of this tile
+        int64_t rows_left = a.n_out - (int64_t)tile * kBatchRows - r;
+        while (it < total) {
             if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
             if (!ok) break;
-            const int64_t row = (int64_t)tile * kBatchRows + r;
             const bool in = step * 4u + (c >> 1) < a.kb;
-            const uint8_t* from = a.codes + row * a.code_pitch + (uint64_t)step * 64u + c * 8u;
+            const uint8_t* src = from + (uint64_t)step * 64u;
+            const uint32_t dst = to + s * stage_bytes;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool ok_row = in && row + 16 * i < a.n_out;
-                const uint8_t* src = ok_row ? from + (int64_t)(16 * i) * a.code_pitch : a.codes;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to + s * stage_bytes + i * 2048u), "l"(src), "r"(ok_row ? 8u : 0u) : "memory");
+                const bool there = in && 16 * i < rows_left;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + i * 2048u), "l"(there ? src : a.codes), "r"(there ? 8u : 0u) : "memory");
+                src += 16 * a.code_pitch;
             }
-            // counts on the stage's barrier once this thread's copies are there; the MMAs' thread makes them visible to the tensor cores
-            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(full + s)) : "memory");
-            next();
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            advance();
+            if (step == 0) { from += kBatchRows * a.code_pitch; rows_left -= kBatchRows; }
+            if (it > (uint32_t)kLag) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
+                announce();
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        while (ok && announced < it) announce();
     } else if (warp == 8) {
-        ScaleQuad now, then;
-        uint32_t tile_of = 0xffffffffu, quad_of = 0;
-        for (uint64_t u = begin; u < end && ok; ++u, ++it) {
-            const uint32_t tile = (uint32_t)(u / a.steps), step = (uint32_t)(u - (uint64_t)tile * a.steps), quad = step / 4u;
-            if (tile != tile_of || quad != quad_of) {     // 16 scales of a row serve four steps; the next ones are requested when these come into use
-                if (tile == tile_of) now = then;
-                else load_scales(now, a.scales, (int64_t)tile * kBatchRows, a.n_out, a.scale_pitch, a.kb, quad, lane);
-                load_scales(then, a.scales, (int64_t)tile * kBatchRows, a.n_out, a.scale_pitch, a.kb, quad + 1, lane);
-                tile_of = tile; quad_of = quad;
+        // boxes of scales are asked for kRawScales ahead; a box is used up when its last word is stored
+        const uint32_t raw = base + kStages * stage_bytes;
+        uint32_t ask_it = 0, ask_tile = tile, ask_step = step, asked = 0, box = 0;
+        auto ask = [&] {
+            if (ask_it >= total) return;
+            if (lane == 0) {
+                mbar_expect(raw_full + asked % kRawScales, kBatchRows * 16u);
+                tma_load_2d(raw + asked % kRawScales * (kBatchRows * 16u), &scale_map, (int)(ask_step / 4u * 16u), (int)(ask_tile * kBatchRows), raw_full + asked % kRawScales);
             }
+            ++asked;
+            const uint32_t steps = min(4u - (ask_step & 3u), a.steps - ask_step);
+            ask_it += steps;
+            ask_step += steps;
+            if (ask_step == a.steps) { ask_step = 0; ++ask_tile; }
+        };
+        for (int e = 0; e < kRawScales; ++e) ask();
+        ScaleQuad now;
+        bool fresh = true;
+        while (it < total) {
+            const uint32_t quad = step / 4u;
+            if (fresh) {
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(raw_full + box % kRawScales, (box / kRawScales) & 1u));
+                if (!ok) break;
+                read_scales(now, raw + box % kRawScales * (kBatchRows * 16u), lane);
+                __syncwarp();
+                ++box;
+                ask();
+            }
+            fresh = (step & 3u) == 3u || step + 1u == a.steps;
             if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
             if (!ok) break;
             const uint32_t at = base + s * stage_bytes + kBatchA + x_bytes;
@@ -257,52 +296,57 @@ mx_batch_kernel(BatchArgs a)
             fence_async_smem();
             __syncwarp();
             if (lane == 0) arrive(full + s);
-            next();
+            advance();
         }
     } else if (warp == 9) {
         if (lane == 0) {
             pdl_wait();
-            for (uint64_t u = begin; u < end && ok; ++u, ++it) {
+            while (it < total) {
                 if (it >= (uint32_t)kStages) ok = mbar_wait(empty + s, phase ^ 1u);
                 if (!ok) break;
                 mbar_expect(full + s, x_bytes);
-                bulk_load(base + s * stage_bytes + kBatchA, a.x_chunks + (u % a.steps) * x_bytes, x_bytes, full + s);
-                next();
+                bulk_load(base + s * stage_bytes + kBatchA, a.x_chunks + (uint64_t)step * x_bytes, x_bytes, full + s);
+                advance();
             }
         }
     } else if (warp == 10) {
-        if (lane == 0) {
-            uint32_t done = 0;
-            for (uint64_t u = begin; u < end && ok; ++done) {
-                const uint64_t stop = min(end, (u / a.steps + 1) * a.steps);
-                if (done > 0) ok = mbar_wait(&acc_empty, (done - 1u) & 1u);
+        uint32_t done = 0;
+        const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + kBatchA), sb0 = smem_desc(base + kBatchA + a.npad * 128u, 0u, 128u),
+                       sa0 = smem_desc(base + kBatchA + x_bytes, 0u, 128u);
+        const uint32_t id0 = instr_desc_mxf4_f8(a.npad, 0), step16 = stage_bytes >> 4;
+        const bool wide = a.npad > 128u;
+        while (it < total && ok) {
+            const uint32_t stop = min(total, it + (a.steps - step));
+            if (done > 0) ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty, (done - 1u) & 1u));
+            for (uint32_t more = 0; it < stop && ok; more = 1u) {
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
+                if (!ok) break;
                 tc_fence_after();
-                for (bool first = true; u < stop && ok; ++u, ++it, first = false) {
-                    ok = mbar_wait_copies(full + s, phase);
-                    if (!ok) break;
-                    fence_async_smem();                   // the codes were copied by the generic proxy
-                    tc_fence_after();
-                    const uint32_t at = base + s * stage_bytes, xb = at + kBatchA, sb = xb + a.npad * 128u, sa = xb + x_bytes;
-                    const uint32_t ta = tmem + 192u + (it & 1u) * 12u, tb = ta + 4u;
-                    scales_to_tmem(ta, sa);
+                const uint32_t off = s * step16, ta = tmem + 192u + (it & 1u) * 12u, tb = ta + 4u;
+                const uint64_t da = da0 + off, db = db0 + off, sb = sb0 + off;
+                if (elect_one()) {
+                    scales_to_tmem(ta, sa0 + off);
                     scales_to_tmem(tb, sb);
-                    if (a.npad > 128u) scales_to_tmem(tb + 4u, sb + kScaleAtom);
-                    const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(xb);
+                    if (wide) scales_to_tmem(tb + 4u, sb + (kScaleAtom >> 4));
 #pragma unroll
                     for (int q = 0; q < 4; ++q)           // 32 columns: 32 bytes on along the rows of either operand, the next byte of the scales
-                        umma_mxf8f6f4(tmem, da + 2 * q, db + 2 * q, instr_desc_mxf4_f8(a.npad, q), ta, tb, !first || q > 0);
+                        umma_mxf8f6f4(tmem, da + 2 * q, db + 2 * q, id0 | (uint32_t)q << 4 | (uint32_t)q << 29, ta, tb, q > 0 ? 1u : more);
                     umma_commit(empty + s);
-                    next();
                 }
-                if (ok) umma_commit(&acc_full);
+                __syncwarp();
+                advance();
             }
+            if (ok && elect_one()) umma_commit(&acc_full);
+            __syncwarp();
+            ++done;
         }
     } else {
         pdl_wait();
         uint32_t done = 0;
-        for (uint64_t u = begin; u < end; ++done) {
-            const uint32_t tile = (uint32_t)(u / a.steps);
-            const uint64_t tile_begin = (uint64_t)tile * a.steps, stop = min(end, tile_begin + a.steps);
+        for (; it < total; ++tile, ++done) {
+            const uint64_t tile_begin = (uint64_t)tile * a.steps;
+            it += a.steps - step;
+            step = 0;
             ok = __all_sync(0xffffffffu, mbar_wait_copies(&acc_full, done & 1u));
             if (!ok) break;
             tc_fence_after();
@@ -310,11 +354,12 @@ mx_batch_kernel(BatchArgs a)
             const bool whole = from == to;
             const int r = warp * 32 + lane;
             const int64_t row = (int64_t)tile * kBatchRows + r;
-            auto slot = [&](uint32_t block) {             // where a block's sums of this tile are: its first tile or its last
-                const bool first = (uint32_t)(share_begin(units, gridDim.x, block) / a.steps) == tile;
-                return a.parts + ((uint64_t)block * 2 + (first ? 0 : 1)) * (uint64_t)(kBatchRows * a.batch) + r;
-            };
+            // where a block's sums of this tile are: slot 0 for its first tile, 1 for its last.  Blocks behind the first of the tile begin in it.
+            const uint64_t slot_floats = (uint64_t)(kBatchRows * a.batch);
+            const uint32_t from_slot = share_begin(units, gridDim.x, from) == tile_begin ? 0u : 1u;
+            auto slot = [&](uint32_t block) { return a.parts + ((uint64_t)block * 2 + (block == from ? from_slot : 0u)) * slot_floats + r; };
             float* part = slot(blockIdx.x);
+            bool odd = false;
             for (int n0 = 0; n0 < a.batch; n0 += 16) {
                 float v[48];
 #pragma unroll
@@ -324,8 +369,8 @@ mx_batch_kernel(BatchArgs a)
                 for (int j = 0; j < 16; ++j) {
                     if (n0 + j >= a.batch) break;
                     const float sum = v[3 * j] + (v[3 * j + 1] + v[3 * j + 2]);
-                    if (whole) put_y(a, row, n0 + j, sum);
-                    else __stcg(part + (n0 + j) * kBatchRows, sum);
+                    if (!whole) __stcg(part + (n0 + j) * kBatchRows, sum);
+                    else if (row < a.n_out) { put_y(a, row, n0 + j, sum); odd |= sum != sum; }
                 }
             }
             tc_fence_before();
@@ -342,21 +387,27 @@ mx_batch_kernel(BatchArgs a)
                     // 16 rows of X at a time, so that their loads overlap
                     for (int n0 = 0; n0 < a.batch; n0 += 16) {
                         float sum[16] = {};
-#pragma unroll 2
-                        for (uint32_t b = from; b <= to; ++b) {
-                            const float* p = slot(b) + n0 * kBatchRows;
+                        for (uint32_t b = from; b <= to; b += 4) {
+                            float v[4][16];
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (n0 + j < a.batch) sum[j] += __ldcg(p + j * kBatchRows);
+                            for (int h = 0; h < 4; ++h) {
+                                const float* p = slot(min(b + h, to)) + n0 * kBatchRows;
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[h][j] = b + h <= to && n0 + j < a.batch ? __ldcg(p + j * kBatchRows) : 0.0f;
+                            }
+#pragma unroll
+                            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) sum[j] += v[h][j];
                         }
 #pragma unroll
                         for (int j = 0; j < 16; ++j)
-                            if (n0 + j < a.batch) put_y(a, row, n0 + j, sum[j]);
+                            if (n0 + j < a.batch && row < a.n_out) { put_y(a, row, n0 + j, sum[j]); odd |= sum[j] != sum[j]; }
                     }
                 }
                 asm volatile("bar.sync 1, 128;" ::: "memory");
             }
-            u = stop;
+            if (odd) mend_row(a, row);
         }
     }
     if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
@@ -369,9 +420,11 @@ mx_batch_kernel(BatchArgs a)
 template <int kStages>
 int launch_batch(const llvq_ctx* ctx, const BatchArgs& a, unsigned grid, cudaStream_t st)
 {
-    const size_t smem = 1024 + (size_t)kStages * ((kBatchA + batch_x_bytes(a.npad) + kScaleAtom + 1023u) & ~1023u);
+    const size_t smem = 1024 + (size_t)kStages * ((kBatchA + batch_x_bytes(a.npad) + kScaleAtom + 1023u) & ~1023u) + kRawScales * kBatchRows * 16;
+    CUtensorMap scale_map;
+    if (!make_byte_map(ctx->device, a.scales, a.scale_pitch, a.n_out, 16, kBatchRows, false, &scale_map)) return LLVQ_ECUDA;
     if (!set_smem<mx_batch_kernel<kStages>>(ctx, smem)) return LLVQ_ECUDA;
-    return launch_pdl(mx_batch_kernel<kStages>, grid, kBatchThreads, smem, st, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    return launch_pdl(mx_batch_kernel<kStages>, grid, kBatchThreads, smem, st, scale_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 }  // namespace
@@ -393,7 +446,9 @@ int mx_batch_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t*
     const uint64_t split = ((uint64_t)a.steps * batch + 7) / 8;
     if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
     if (launch_pdl(mx_batch_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
-    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles * a.steps, (uint64_t)ctx->sm_count);
+    // A thread block per SM, or, where that uses five sixths of them at least, so many that each has part of one tile only.
+    const uint64_t sms = (uint64_t)ctx->sm_count, apart = a.tiles <= sms ? sms / a.tiles * a.tiles : 0;
+    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles * a.steps, apart * 6 >= sms * 5 ? apart : sms);
     // as many stages as shared memory holds
     if (a.npad <= 48) return launch_batch<9>(ctx, a, grid, st);
     if (a.npad <= 96) return launch_batch<7>(ctx, a, grid, st);

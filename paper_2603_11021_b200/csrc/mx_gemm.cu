@@ -10,9 +10,9 @@ using namespace llvq;
 // tcgen05.mma.kind::mxf4 takes e2m1 operands from shared memory and one e8m0 scale per row and 32 columns from tensor memory: nothing of
 // either operand passes through registers.  A thread block computes tiles of 128 rows of W (the lanes of tensor memory) by kBn tokens
 // (its columns), 256 columns of both operands (128 bytes of codes per row) per stage:
-//   warp 0      copies codes with TMA (swizzled rows of 128 bytes; what lies past the matrix reads as zero)
+//   warp 0      copies codes with TMA (swizzled rows of 128 bytes; what lies past the matrix reads as zero), and scales, 16 per row at a time
 //   warps 2, 3  lay the scales of W and X out as tcgen05.cp wants them: of 128 rows and 4 blocks, 512 bytes, row r at 16 (r % 32) + 4 (r / 32).
-//               A lane loads 16 scales of four rows 32 apart (16 bytes each: that is what the rows' padding is for) and stores four times 16 bytes
+//               A lane reads 16 scales of four rows 32 apart (the rows' padding is for that) and stores four times 16 bytes in two stages
 //   warp 1      copies the scales to tensor memory and issues four MMAs of 64 columns per stage
 //   warps 4-11  take the accumulator out as bf16 (a quarter of the lanes by half of the columns each), hand it back, then write Y
 // There is one accumulator: taking it out costs the tensor cores a few hundred of the thousands of cycles of a tile.
@@ -28,14 +28,15 @@ template <int kBn> struct MmShape {
     static constexpr int kStages = kBn == 256 ? 4 : kBn == 128 ? 6 : 8;
     static constexpr uint32_t kScaleCols = 8 + 8 * kBHalves;      // columns of tensor memory that a stage's scales take
     static constexpr uint32_t kTmem = kBn == 256 ? 512 : kBn == 128 ? 256 : 128;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + 256;
+    static constexpr int kRawEntries = kStages / 2 + 1;   // boxes of scales as they come, of two stages each
+    static constexpr uint32_t kRaw = (kMmRows + kBn) * 16;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kRawEntries * kRaw + 256;
     static_assert(kStage % 1024 == 0 && kBn + 2 * kScaleCols <= kTmem && kSmem <= 227 * 1024, "");
 };
 
 struct MmArgs {
-    const uint8_t *w_scales, *x_scales;
     int64_t n_out, tokens;
-    uint32_t kb, pitch, k_stages;                         // blocks per row, bytes per row of scales, stages per tile
+    uint32_t kb, k_stages;                                // blocks per row, stages per tile
     uint32_t tiles_m, tiles_n;
     __nv_bfloat16* y;
     uint32_t* flags;
@@ -79,19 +80,23 @@ __device__ __forceinline__ void mm_tile(const MmArgs& a, uint32_t tile, uint32_t
 
 template <int kBn>
 __global__ void __launch_bounds__(kMmThreads, 1)
-mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, MmArgs a)
+mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap ws_map,
+               const __grid_constant__ CUtensorMap xs_map, MmArgs a)
 {
     using S = MmShape<kBn>;
     extern __shared__ uint8_t mm_smem[];
     const uint32_t base = (smem_u32(mm_smem) + 1023u) & ~1023u;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(mm_smem + (base - smem_u32(mm_smem)) + S::kStages * S::kStage);
-    uint64_t *full = bars, *empty = bars + S::kStages, *acc_full = bars + 2 * S::kStages, *acc_empty = acc_full + 1;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(mm_smem + (base - smem_u32(mm_smem)) + S::kStages * S::kStage + S::kRawEntries * S::kRaw);
+    uint64_t *full = bars, *empty = bars + S::kStages, *acc_full = bars + 2 * S::kStages, *acc_empty = acc_full + 1, *raw_full = acc_empty + 1,
+             *raw_empty = raw_full + S::kRawEntries;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(raw_empty + S::kRawEntries);
+    const uint32_t raw = base + S::kStages * S::kStage;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + s, 3); mbar_init(empty + s, 1); }      // TMA, scales of W, scales of X
+        for (int e = 0; e < S::kRawEntries; ++e) { mbar_init(raw_full + e, 1); mbar_init(raw_empty + e, 2); }
         mbar_init(acc_full, 1);
         mbar_init(acc_empty, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -107,11 +112,20 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t it = 0;
+            uint32_t it = 0, pair = 0;
             for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
                 uint32_t m, n;
                 mm_tile(a, tile, m, n);
                 for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
+                    if ((k & 1u) == 0u) {
+                        const uint32_t e = pair % S::kRawEntries, turn = pair / S::kRawEntries;
+                        if (turn > 0) ok = mbar_wait(raw_empty + e, (turn - 1u) & 1u);
+                        if (!ok) break;
+                        mbar_expect(raw_full + e, S::kRaw);
+                        tma_load_2d(raw + e * S::kRaw, &ws_map, (int)(k * 8u), (int)(m * kMmRows), raw_full + e);
+                        tma_load_2d(raw + e * S::kRaw + kMmRows * 16u, &xs_map, (int)(k * 8u), (int)(n * kBn), raw_full + e);
+                        ++pair;
+                    }
                     const uint32_t s = it % S::kStages, round = it / S::kStages;
                     if (round > 0) ok = mbar_wait(empty + s, (round - 1u) & 1u);
                     if (!ok) break;
@@ -123,52 +137,53 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t it = 0, done = 0;
-            for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++done) {
-                if (done > 0) ok = mbar_wait(acc_empty, (done - 1u) & 1u);
+        uint32_t done = 0, s = 0, phase = 0, buffer = 0;
+        const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + S::kA), sc0 = smem_desc(base + S::kA + S::kB, 0u, 128u);
+        for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++done) {
+            if (done > 0) ok = __all_sync(0xffffffffu, mbar_wait(acc_empty, (done - 1u) & 1u));
+            for (uint32_t k = 0; k < a.k_stages && ok; ++k) {
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
+                if (!ok) break;
                 tc_fence_after();
-                for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
-                    const uint32_t s = it % S::kStages;
-                    ok = mbar_wait_copies(full + s, (it / S::kStages) & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t at = base + s * S::kStage, sa = at + S::kA + S::kB, sb = sa + 2 * kScaleAtom;
-                    const uint32_t ta = tmem + kBn + (it & 1u) * S::kScaleCols, tb = ta + 8;
+                const uint32_t off = s * (S::kStage >> 4), ta = tmem + kBn + buffer * S::kScaleCols, tb = ta + 8;
+                const uint64_t da = da0 + off, db = db0 + off, sc = sc0 + off;
+                if (elect_one()) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        scales_to_tmem(ta + 4 * h, sa + h * kScaleAtom);
+                        scales_to_tmem(ta + 4 * h, sc + h * (kScaleAtom >> 4));
 #pragma unroll
-                        for (int g = 0; g < S::kBHalves; ++g) scales_to_tmem(tb + h * 4 * S::kBHalves + 4 * g, sb + (g * 2 + h) * kScaleAtom);
+                        for (int g = 0; g < S::kBHalves; ++g) scales_to_tmem(tb + h * 4 * S::kBHalves + 4 * g, sc + (2 + g * 2 + h) * (kScaleAtom >> 4));
                     }
-                    const uint64_t da = smem_desc_sw128(at), db = smem_desc_sw128(at + S::kA);
 #pragma unroll
                     for (int q = 0; q < 4; ++q)           // 64 columns: 32 bytes on along the rows, two blocks on along the scales
                         umma_mxf4(tmem, da + 2 * q, db + 2 * q, instr_desc_mxf4(kBn, q & 1), ta + 4 * (q >> 1), tb + 4 * S::kBHalves * (q >> 1), k > 0 || q > 0);
                     umma_commit(empty + s);
                 }
-                if (ok) umma_commit(acc_full);
+                __syncwarp();
+                buffer ^= 1u;
+                if (++s == (uint32_t)S::kStages) { s = 0; phase ^= 1u; }
             }
+            if (ok && elect_one()) umma_commit(acc_full);
+            __syncwarp();
         }
     } else if (warp < 4) {
         const bool of_w = warp == 2;
-        const uint8_t* scales = of_w ? a.w_scales : a.x_scales;
-        const int64_t rows = of_w ? a.n_out : a.tokens;
+        const uint32_t from = raw + (of_w ? 0u : kMmRows * 16u);
         constexpr int kGroups = S::kBHalves;              // W has one group of 128 rows
-        uint32_t it = 0;
+        uint32_t it = 0, pair = 0;
         for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-            uint32_t m, n;
-            mm_tile(a, tile, m, n);
-            const int64_t row0 = of_w ? (int64_t)m * kMmRows : (int64_t)n * kBn;
-            ScaleQuad now[kGroups], next[kGroups];
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g)
-                if (g == 0 || !of_w) load_scales(now[g], scales, row0 + 128 * g, rows, a.pitch, a.kb, 0, lane);
+            ScaleQuad now[kGroups];
             for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
                 if ((k & 1u) == 0u) {
+                    const uint32_t e = pair % S::kRawEntries;
+                    ok = __all_sync(0xffffffffu, mbar_wait_copies(raw_full + e, (pair / S::kRawEntries) & 1u));
+                    if (!ok) break;
 #pragma unroll
                     for (int g = 0; g < kGroups; ++g)
-                        if (g == 0 || !of_w) load_scales(next[g], scales, row0 + 128 * g, rows, a.pitch, a.kb, k / 2 + 1, lane);
+                        if (g == 0 || !of_w) read_scales(now[g], from + e * S::kRaw + g * 2048u, lane);
+                    __syncwarp();
+                    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(raw_empty + e)) : "memory");
+                    ++pair;
                 }
                 const uint32_t s = it % S::kStages, round = it / S::kStages;
                 if (round > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, (round - 1u) & 1u));
@@ -184,7 +199,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                     } else {
                         store_scales<2>(to, now[g], a.kb, first, lane);
                         store_scales<3>(to + kScaleAtom, now[g], a.kb, first, lane);
-                        now[g] = next[g];
                     }
                 }
                 fence_async_smem();
@@ -225,15 +239,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
 }
 
 template <int kBn>
-int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* w_codes, int64_t pitch, MmArgs a, cudaStream_t st)
+int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t k_in, MmArgs a,
+                   cudaStream_t st)
 {
-    CUtensorMap w_map, x_map;
+    CUtensorMap w_map, x_map, ws_map, xs_map;
+    const int64_t pitch = mx_code_pitch(k_in), scale_pitch = mx_scale_pitch(k_in);
+    if (!make_byte_map(ctx->device, w_scales, scale_pitch, a.n_out, 16, kMmRows, false, &ws_map) ||
+        !make_byte_map(ctx->device, x_scales, scale_pitch, a.tokens, 16, kBn, false, &xs_map)) return LLVQ_ECUDA;
     if (!make_byte_map(ctx->device, w_codes, pitch, a.n_out, (int)kStageCodes, kMmRows, true, &w_map) ||
         !make_byte_map(ctx->device, x_codes, pitch, a.tokens, (int)kStageCodes, kBn, true, &x_map)) return LLVQ_ECUDA;
     if (!set_smem<mx_gemm_kernel<kBn>>(ctx, MmShape<kBn>::kSmem)) return LLVQ_ECUDA;
     a.tiles_n = (uint32_t)((a.tokens + kBn - 1) / kBn);
     const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles_m * a.tiles_n, (uint64_t)ctx->sm_count);
-    return launch_pdl(mx_gemm_kernel<kBn>, grid, kMmThreads, MmShape<kBn>::kSmem, st, w_map, x_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    return launch_pdl(mx_gemm_kernel<kBn>, grid, kMmThreads, MmShape<kBn>::kSmem, st, w_map, x_map, ws_map, xs_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 }  // namespace
@@ -252,7 +270,7 @@ extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const
     cudaStream_t st = (cudaStream_t)stream;
     if (k_in == 0) return cudaMemsetAsync(d_y_bf16, 0, (size_t)n_out * tokens * 2, st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
     MmArgs a{};
-    a.w_scales = d_scales; a.x_scales = d_x_scales; a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in); a.pitch = (uint32_t)mx_scale_pitch(k_in);
+    a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in);
     a.k_stages = (a.kb + 7) / 8; a.tiles_m = (uint32_t)((n_out + kMmRows - 1) / kMmRows); a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
     // The widest tile whose rounds over the SMs take least: a stage takes about 128 / 64 / 48 cycles per 64 columns with 256 / 128 / 64 tokens
     // (the narrowest is held up by its reads of shared memory).
@@ -261,8 +279,7 @@ extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const
         return (t + ctx->sm_count - 1) / ctx->sm_count * cycles;
     };
     const uint64_t c256 = cost(256, 128), c128 = cost(128, 64), c64 = cost(64, 48);
-    const int64_t pitch = mx_code_pitch(k_in);
-    if (c256 <= c128 && c256 <= c64) return launch_mx_gemm<256>(ctx, d_x_codes, d_codes, pitch, a, st);
-    if (c128 <= c64) return launch_mx_gemm<128>(ctx, d_x_codes, d_codes, pitch, a, st);
-    return launch_mx_gemm<64>(ctx, d_x_codes, d_codes, pitch, a, st);
+    if (c256 <= c128 && c256 <= c64) return launch_mx_gemm<256>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
+    if (c128 <= c64) return launch_mx_gemm<128>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
+    return launch_mx_gemm<64>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
 }

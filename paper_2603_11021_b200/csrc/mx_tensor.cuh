@@ -8,21 +8,31 @@ namespace llvq {
 
 constexpr uint32_t kScaleAtom = 512;                      // scales of 128 rows and 4 blocks: row r at 16 (r % 32) + 4 (r / 32), block j at byte j
 
-// 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t smem)
+// One lane of a warp whose lanes are all here.  Loops that issue MMAs are run by the whole warp and only the instructions themselves by this lane, so
+// that their operands stay in uniform registers: in a branch on the lane's number every operand is moved there for each instruction.
+__device__ __forceinline__ bool elect_one()
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(smem_desc(smem, 0u, 128u)) : "memory");
+    uint32_t is;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+    return is != 0u;
 }
 
-// 16 scales (blocks 16 p .. 16 p + 15) of the rows l, l + 32, l + 64, l + 96 of a group of 128 that starts at row0; zero outside the matrix.
+// The warp's number, known to the compiler to be the same for all its lanes.
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
+
+// 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc)      // desc = smem_desc(address, 0, 128)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// 16 scales (16 neighbouring blocks) of the rows l, l + 32, l + 64, l + 96 of 128, from a box of rows of 16 bytes in shared memory.
 struct ScaleQuad { uint4 v[4]; };
-__device__ __forceinline__ void load_scales(ScaleQuad& q, const uint8_t* scales, int64_t row0, int64_t rows, uint32_t pitch, uint32_t kb, uint32_t p, int lane)
+__device__ __forceinline__ void read_scales(ScaleQuad& q, uint32_t smem, int lane)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = row0 + lane + 32 * i;
-        q.v[i] = row < rows && 16u * p < kb ? __ldg(reinterpret_cast<const uint4*>(scales + row * pitch) + p) : make_uint4(0u, 0u, 0u, 0u);
-    }
+    for (int i = 0; i < 4; ++i)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(q.v[i].x), "=r"(q.v[i].y), "=r"(q.v[i].z), "=r"(q.v[i].w) : "r"(smem + (lane + 32 * i) * 16) : "memory");
 }
 
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
