@@ -17,16 +17,21 @@ using namespace llvq;
 // A row of X is three columns of the product, added up in binary32 at the end.
 //
 // First kernel: the three terms of X, laid out as the second copies them (chunks of 128 columns: rows of 128 bytes, swizzled, then their scales),
-// once for all thread blocks.  Second kernel: tiles of 128 rows of W by all of X.  The steps of 128 columns of all tiles are dealt out evenly in one
-// line, so every SM reads the same share of W whatever the shape; a tile that several thread blocks share is added up by whichever
-// is done last, in the order of the blocks.
-//   warps 4-7   copy codes with cp.async, 8 bytes (16 elements) into every 16 of shared memory: the form in which the instruction takes 4-bit operands
-//   warp 8      the scales of W    warp 9: X    warp 10: the MMAs, four per stage    warps 0-3: the accumulator and Y
+// once for all thread blocks.  Second kernel: tiles of 256 rows of W (two accumulators that share what is read of X) by all of X.  The steps of
+// 128 columns of all tiles are dealt out evenly in one line, so every SM reads the same share of W whatever the shape; a tile that several
+// thread blocks share is added up by whichever is done last, in the order of the blocks.
+//   warp 17     codes, as they are, with TMA: 64 bytes of 256 rows per step, kBatchPacked steps ahead
+//   warps 8-15  two groups of four, every other step each: 8 bytes (16 elements) of codes to every 16 bytes of the operand: the form in which the
+//               instruction takes 4-bit operands
+//   warp 16     the scales of W    warp 18: X    warp 19: the MMAs, eight per step    warps 0-7: the accumulators and Y
 // It begins to read W while the first kernel still runs (which waits for everything before it first).
-// Bound by HBM for few rows of X; at 64 the products take as long as the reads.
-constexpr int kBatchRows = 128, kBatchCols = 128, kBatchThreads = 352;
-constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a stage's weights, a byte of room per element
-constexpr int kRawScales = 4;                             // boxes of scales under way: 128 rows, 16 blocks, for four steps each
+// Bound by HBM for few rows of X; at 64 the products, and reading X out of L2 for every tile, take as long.
+constexpr int kBatchRows = 256, kBatchCols = 128, kBatchThreads = 640;
+constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a step's weights as operand, a byte of room per element
+constexpr uint32_t kBatchCode = kBatchA / 2;              // and as they are stored
+constexpr int kBatchPacked = 4, kBatchX = 3;              // steps of codes and of X in shared memory; of operands 3 for up to 32 rows of X, else 2
+static_assert(kBatchPacked % 2 == 0, "");                 // a place in the ring of codes belongs to one of the two groups: each sees every phase of its barriers
+constexpr int kRawScales = 3;                             // boxes of scales under way: 256 rows, 16 blocks, for four steps each
 
 __host__ __device__ inline uint32_t batch_npad(int batch) { return (3u * (uint32_t)batch + 15u) / 16u * 16u; }
 __host__ __device__ inline uint32_t batch_x_bytes(uint32_t npad) { return npad * 128u + 2u * kScaleAtom; }      // of a chunk
@@ -55,7 +60,7 @@ struct BatchArgs {
     const __nv_bfloat16* x;
     int batch;
     bool x_quads;                                         // four elements of X may be loaded at once
-    uint32_t npad;
+    uint32_t npad, stages;
     uint8_t* x_chunks;
     uint32_t* counters;
     uint8_t* notes;
@@ -186,154 +191,180 @@ __device__ __noinline__ void mend_row(const BatchArgs& a, int64_t row)
     }
 }
 
-template <int kStages>
+// A place in a ring of n and its phase.
+struct Ring {
+    uint32_t at = 0, phase = 0;
+    __device__ __forceinline__ void next(uint32_t n, uint32_t by = 1u) { at += by; if (at >= n) { at -= n; phase ^= 1u; } }
+};
+
 __global__ void __launch_bounds__(kBatchThreads, 1)
-mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
+mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
 {
-    constexpr int kLag = (kStages + 1) / 2;               // copies of codes are announced when kLag later ones are under way: the other stages keep the MMAs fed
+    constexpr uint32_t kStage = kBatchA + 1024u;          // a step's weights and their scales
     extern __shared__ uint8_t mb_smem[];
-    __shared__ uint64_t full[kStages], empty[kStages], raw_full[kRawScales], acc_full, acc_empty;
+    __shared__ uint64_t code_full[kBatchPacked], code_empty[kBatchPacked], full[3], empty[3], x_full[kBatchX], x_empty[kBatchX], raw_full[kRawScales], acc_full, acc_empty;
     __shared__ uint32_t tmem_slot, last_slot;
-    const uint32_t base = (smem_u32(mb_smem) + 1023u) & ~1023u;
-    const uint32_t x_bytes = batch_x_bytes(a.npad), stage_bytes = (kBatchA + x_bytes + kScaleAtom + 1023u) & ~1023u;
+    const uint32_t base = (smem_u32(mb_smem) + 1023u) & ~1023u, stages = a.stages;
+    const uint32_t x_bytes = batch_x_bytes(a.npad), codes = base + stages * kStage, raw = codes + kBatchPacked * kBatchCode, x_at = raw + kRawScales * kBatchRows * 16u;
     const int warp = warp_number(), lane = threadIdx.x & 31;
     const uint64_t units = (uint64_t)a.tiles * a.steps, begin = share_begin(units, gridDim.x, blockIdx.x), end = share_begin(units, gridDim.x, blockIdx.x + 1);
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full + s, 4 + 2); mbar_init(empty + s, 1); }       // four warps' copies of codes, scales, X
+        for (int e = 0; e < kBatchPacked; ++e) { mbar_init(code_full + e, 1); mbar_init(code_empty + e, 4); }
+        for (int e = 0; e < 3; ++e) { mbar_init(full + e, 4 + 1); mbar_init(empty + e, 1); }        // four warps of codes, scales
+        for (int e = 0; e < kBatchX; ++e) { mbar_init(x_full + e, 1); mbar_init(x_empty + e, 1); }
         for (int e = 0; e < kRawScales; ++e) mbar_init(raw_full + e, 1);
         mbar_init(&acc_full, 1);
-        mbar_init(&acc_empty, 4);
+        mbar_init(&acc_empty, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 10) tmem_alloc(&tmem_slot, 256);
+    if (warp == 19) tmem_alloc(&tmem_slot, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     bool ok = true;
-    uint32_t s = 0, phase = 0;
-    auto next = [&] { if (++s == (uint32_t)kStages) { s = 0; phase ^= 1u; } };
     const uint32_t total = (uint32_t)(end - begin);
-    uint32_t tile = (uint32_t)(begin / a.steps), step = (uint32_t)(begin - (uint64_t)tile * a.steps), it = 0;      // it: stages so far
-    auto advance = [&] { ++it; next(); if (++step == a.steps) { step = 0; ++tile; } };
+    uint32_t tile = (uint32_t)(begin / a.steps), step = (uint32_t)(begin - (uint64_t)tile * a.steps), it = 0;      // it: steps so far
+    auto advance = [&] { ++it; if (++step == a.steps) { step = 0; ++tile; } };
 
-    if (warp >= 4 && warp < 8) {
-        const uint32_t p = threadIdx.x - 128u, c = p & 7u, r = p >> 3;          // container of a row; rows r, r + 16, ...
-        const uint32_t to = base + r * 128u + ((c ^ (r & 7u)) << 4);
-        uint32_t announced = 0, at = 0;
-        auto announce = [&] {                             // what this warp has copied for the next stage becomes visible to the tensor cores
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) arrive(full + at);
-            ++announced;
-            if (++at == (uint32_t)kStages) at = 0;
-        };
-        const uint8_t* from = a.codes + ((int64_t)tile * kBatchRows + r) * a.code_pitch + c * 8u;      // of this tile
-        int64_t rows_left = a.n_out - (int64_t)tile * kBatchRows - r;
-        while (it < total) {
-            if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
+    if (warp >= 8 && warp < 16) {
+        const uint32_t p = threadIdx.x & 127u, j = p & 3u, r = p >> 2;      // 16 bytes of a row; rows r, r + 32, ...
+        const uint32_t to = r * 128u + (((2u * j) ^ (r & 7u)) << 4);      // the second half's place differs in the lowest bit
+        Ring in, out;
+        it = (uint32_t)(warp - 8) >> 2;
+        in.next(kBatchPacked, it);
+        out.next(stages, it);
+        for (; it < total; it += 2) {
+            ok = __all_sync(0xffffffffu, mbar_wait_copies(code_full + in.at, in.phase));
             if (!ok) break;
-            const bool in = step * 4u + (c >> 1) < a.kb;
-            const uint8_t* src = from + (uint64_t)step * 64u;
-            const uint32_t dst = to + s * stage_bytes;
+            uint4 v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(codes + in.at * kBatchCode + p * 16u + i * 2048u) : "memory");
+            __syncwarp();
+            if (lane == 0) arrive(code_empty + in.at);
+            if (it >= stages) ok = __all_sync(0xffffffffu, mbar_wait(empty + out.at, out.phase ^ 1u));
+            if (!ok) break;
+            const uint32_t at = base + out.at * kStage + to;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool there = in && 16 * i < rows_left;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + i * 2048u), "l"(there ? src : a.codes), "r"(there ? 8u : 0u) : "memory");
-                src += 16 * a.code_pitch;
+                asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"(at + i * 4096u), "r"(v[i].x), "r"(v[i].y) : "memory");
+                asm volatile("st.shared.v2.b32 [%0], {%1,%2};" ::"r"((at ^ 16u) + i * 4096u), "r"(v[i].z), "r"(v[i].w) : "memory");
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            advance();
-            if (step == 0) { from += kBatchRows * a.code_pitch; rows_left -= kBatchRows; }
-            if (it > (uint32_t)kLag) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(kLag) : "memory");
-                announce();
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) arrive(full + out.at);
+            in.next(kBatchPacked, 2u);
+            out.next(stages, 2u);
+        }
+    } else if (warp == 17) {
+        if (lane == 0) {
+            Ring e;
+            while (it < total) {
+                if (it >= (uint32_t)kBatchPacked) ok = mbar_wait(code_empty + e.at, e.phase ^ 1u);
+                if (!ok) break;
+                mbar_expect(code_full + e.at, kBatchCode);
+                tma_load_2d(codes + e.at * kBatchCode, &code_map, (int)(step * 64u), (int)(tile * kBatchRows), code_full + e.at);
+                e.next(kBatchPacked);
+                advance();
             }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        while (ok && announced < it) announce();
-    } else if (warp == 8) {
-        // boxes of scales are asked for kRawScales ahead; a box is used up when its last word is stored
-        const uint32_t raw = base + kStages * stage_bytes;
-        uint32_t ask_it = 0, ask_tile = tile, ask_step = step, asked = 0, box = 0;
+    } else if (warp == 16) {
+        // boxes of scales are asked for kRawScales ahead; a box is in registers while its four words are stored
+        uint32_t ask_it = 0, ask_tile = tile, ask_step = step;
+        Ring asked, box, out;
         auto ask = [&] {
             if (ask_it >= total) return;
             if (lane == 0) {
-                mbar_expect(raw_full + asked % kRawScales, kBatchRows * 16u);
-                tma_load_2d(raw + asked % kRawScales * (kBatchRows * 16u), &scale_map, (int)(ask_step / 4u * 16u), (int)(ask_tile * kBatchRows), raw_full + asked % kRawScales);
+                mbar_expect(raw_full + asked.at, kBatchRows * 16u);
+                tma_load_2d(raw + asked.at * (kBatchRows * 16u), &scale_map, (int)(ask_step / 4u * 16u), (int)(ask_tile * kBatchRows), raw_full + asked.at);
             }
-            ++asked;
+            asked.next(kRawScales);
             const uint32_t steps = min(4u - (ask_step & 3u), a.steps - ask_step);
             ask_it += steps;
             ask_step += steps;
             if (ask_step == a.steps) { ask_step = 0; ++ask_tile; }
         };
         for (int e = 0; e < kRawScales; ++e) ask();
-        ScaleQuad now;
+        ScaleQuad now[2];
         bool fresh = true;
         while (it < total) {
             const uint32_t quad = step / 4u;
             if (fresh) {
-                ok = __all_sync(0xffffffffu, mbar_wait_copies(raw_full + box % kRawScales, (box / kRawScales) & 1u));
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(raw_full + box.at, box.phase));
                 if (!ok) break;
-                read_scales(now, raw + box % kRawScales * (kBatchRows * 16u), lane);
+                read_scales(now[0], raw + box.at * (kBatchRows * 16u), lane);
+                read_scales(now[1], raw + box.at * (kBatchRows * 16u) + 2048u, lane);
                 __syncwarp();
-                ++box;
+                box.next(kRawScales);
                 ask();
             }
             fresh = (step & 3u) == 3u || step + 1u == a.steps;
-            if (it >= (uint32_t)kStages) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, phase ^ 1u));
+            if (it >= stages) ok = __all_sync(0xffffffffu, mbar_wait(empty + out.at, out.phase ^ 1u));
             if (!ok) break;
-            const uint32_t at = base + s * stage_bytes + kBatchA + x_bytes;
-            switch (step & 3u) {
-                case 0: store_scales<0>(at, now, a.kb, quad * 16u, lane); break;
-                case 1: store_scales<1>(at, now, a.kb, quad * 16u, lane); break;
-                case 2: store_scales<2>(at, now, a.kb, quad * 16u, lane); break;
-                default: store_scales<3>(at, now, a.kb, quad * 16u, lane);
+            const uint32_t at = base + out.at * kStage + kBatchA;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t half = at + h * kScaleAtom;
+                switch (step & 3u) {
+                    case 0: store_scales<0>(half, now[h], a.kb, quad * 16u, lane); break;
+                    case 1: store_scales<1>(half, now[h], a.kb, quad * 16u, lane); break;
+                    case 2: store_scales<2>(half, now[h], a.kb, quad * 16u, lane); break;
+                    default: store_scales<3>(half, now[h], a.kb, quad * 16u, lane);
+                }
             }
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) arrive(full + s);
+            if (lane == 0) arrive(full + out.at);
+            out.next(stages);
             advance();
         }
-    } else if (warp == 9) {
+    } else if (warp == 18) {
         if (lane == 0) {
             pdl_wait();
+            Ring e;
             while (it < total) {
-                if (it >= (uint32_t)kStages) ok = mbar_wait(empty + s, phase ^ 1u);
+                if (it >= (uint32_t)kBatchX) ok = mbar_wait(x_empty + e.at, e.phase ^ 1u);
                 if (!ok) break;
-                mbar_expect(full + s, x_bytes);
-                bulk_load(base + s * stage_bytes + kBatchA, a.x_chunks + (uint64_t)step * x_bytes, x_bytes, full + s);
+                mbar_expect(x_full + e.at, x_bytes);
+                bulk_load(x_at + e.at * x_bytes, a.x_chunks + (uint64_t)step * x_bytes, x_bytes, x_full + e.at);
+                e.next(kBatchX);
                 advance();
             }
         }
-    } else if (warp == 10) {
+    } else if (warp == 19) {
         uint32_t done = 0;
-        const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + kBatchA), sb0 = smem_desc(base + kBatchA + a.npad * 128u, 0u, 128u),
-                       sa0 = smem_desc(base + kBatchA + x_bytes, 0u, 128u);
-        const uint32_t id0 = instr_desc_mxf4_f8(a.npad, 0), step16 = stage_bytes >> 4;
+        Ring in, x;
+        const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(x_at), sa0 = smem_desc(base + kBatchA, 0u, 128u), sb0 = smem_desc(x_at + a.npad * 128u, 0u, 128u);
+        const uint32_t id0 = instr_desc_mxf4_f8(a.npad, 0), x16 = x_bytes >> 4;
         const bool wide = a.npad > 128u;
         while (it < total && ok) {
             const uint32_t stop = min(total, it + (a.steps - step));
             if (done > 0) ok = __all_sync(0xffffffffu, mbar_wait(&acc_empty, (done - 1u) & 1u));
             for (uint32_t more = 0; it < stop && ok; more = 1u) {
-                ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
+                ok = __all_sync(0xffffffffu, mbar_wait_copies(x_full + x.at, x.phase) && mbar_wait_copies(full + in.at, in.phase));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t off = s * step16, ta = tmem + 192u + (it & 1u) * 12u, tb = ta + 4u;
-                const uint64_t da = da0 + off, db = db0 + off, sb = sb0 + off;
+                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + (it & 1u) * 16u, tb = ta + 8u;
+                const uint64_t da = da0 + off, db = db0 + x_off, sa = sa0 + off, sb = sb0 + x_off;
                 if (elect_one()) {
-                    scales_to_tmem(ta, sa0 + off);
+                    scales_to_tmem(ta, sa);
+                    scales_to_tmem(ta + 4u, sa + (kScaleAtom >> 4));
                     scales_to_tmem(tb, sb);
                     if (wide) scales_to_tmem(tb + 4u, sb + (kScaleAtom >> 4));
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)           // 32 columns: 32 bytes on along the rows of either operand, the next byte of the scales
-                        umma_mxf8f6f4(tmem, da + 2 * q, db + 2 * q, id0 | (uint32_t)q << 4 | (uint32_t)q << 29, ta, tb, q > 0 ? 1u : more);
-                    umma_commit(empty + s);
+                    for (int h = 0; h < 2; ++h)           // rows 0-127 and 128-255 of the tile
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)       // 32 columns: 32 bytes on along the rows of either operand, the next byte of the scales
+                            umma_mxf8f6f4(tmem + 192u * h, da + 1024u * h + 2 * q, db + 2 * q, id0 | (uint32_t)q << 4 | (uint32_t)q << 29, ta + 4u * h, tb, q > 0 ? 1u : more);
+                    umma_commit(empty + in.at);
+                    umma_commit(x_empty + x.at);
                 }
                 __syncwarp();
+                in.next(stages);
+                x.next(kBatchX);
                 advance();
             }
             if (ok && elect_one()) umma_commit(&acc_full);
@@ -354,6 +385,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
             const bool whole = from == to;
             const int r = warp * 32 + lane;
             const int64_t row = (int64_t)tile * kBatchRows + r;
+            const uint32_t acc = tmem + ((uint32_t)(warp & 3) << 21) + (warp >= 4 ? 192u : 0u);
             // where a block's sums of this tile are: slot 0 for its first tile, 1 for its last.  Blocks behind the first of the tile begin in it.
             const uint64_t slot_floats = (uint64_t)(kBatchRows * a.batch);
             const uint32_t from_slot = share_begin(units, gridDim.x, from) == tile_begin ? 0u : 1u;
@@ -364,7 +396,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
                 float v[48];
 #pragma unroll
                 for (int h = 0; h < 3; ++h)
-                    if (3u * n0 + 16u * h < a.npad) tmem_ld16(tmem + ((uint32_t)warp << 21) + 3u * n0 + 16u * h, v + 16 * h);
+                    if (3u * n0 + 16u * h < a.npad) tmem_ld16(acc + 3u * n0 + 16u * h, v + 16 * h);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
                     if (n0 + j >= a.batch) break;
@@ -378,25 +410,25 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
             if (lane == 0) arrive(&acc_empty);
             if (!whole) {                                 // the last of the blocks that share the tile adds their sums up
                 __threadfence();
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                asm volatile("bar.sync 1, 256;" ::: "memory");
                 if (threadIdx.x == 0) last_slot = atomicAdd(a.counters + tile, 1u) == to - from;
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                asm volatile("bar.sync 1, 256;" ::: "memory");
                 const bool last = last_slot != 0u;
                 if (last) {
                     __threadfence();
-                    // 16 rows of X at a time, so that their loads overlap
+                    // 16 rows of X of two blocks at a time, so that their loads overlap
                     for (int n0 = 0; n0 < a.batch; n0 += 16) {
                         float sum[16] = {};
-                        for (uint32_t b = from; b <= to; b += 4) {
-                            float v[4][16];
+                        for (uint32_t b = from; b <= to; b += 2) {
+                            float v[2][16];
 #pragma unroll
-                            for (int h = 0; h < 4; ++h) {
+                            for (int h = 0; h < 2; ++h) {
                                 const float* p = slot(min(b + h, to)) + n0 * kBatchRows;
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) v[h][j] = b + h <= to && n0 + j < a.batch ? __ldcg(p + j * kBatchRows) : 0.0f;
                             }
 #pragma unroll
-                            for (int h = 0; h < 4; ++h)
+                            for (int h = 0; h < 2; ++h)
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) sum[j] += v[h][j];
                         }
@@ -405,7 +437,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
                             if (n0 + j < a.batch && row < a.n_out) { put_y(a, row, n0 + j, sum[j]); odd |= sum[j] != sum[j]; }
                     }
                 }
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                asm volatile("bar.sync 1, 256;" ::: "memory");
             }
             if (odd) mend_row(a, row);
         }
@@ -414,17 +446,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap scale_map, BatchArgs a)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 10) tmem_dealloc(tmem, 256);
-}
-
-template <int kStages>
-int launch_batch(const llvq_ctx* ctx, const BatchArgs& a, unsigned grid, cudaStream_t st)
-{
-    const size_t smem = 1024 + (size_t)kStages * ((kBatchA + batch_x_bytes(a.npad) + kScaleAtom + 1023u) & ~1023u) + kRawScales * kBatchRows * 16;
-    CUtensorMap scale_map;
-    if (!make_byte_map(ctx->device, a.scales, a.scale_pitch, a.n_out, 16, kBatchRows, false, &scale_map)) return LLVQ_ECUDA;
-    if (!set_smem<mx_batch_kernel<kStages>>(ctx, smem)) return LLVQ_ECUDA;
-    return launch_pdl(mx_batch_kernel<kStages>, grid, kBatchThreads, smem, st, scale_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    if (warp == 19) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace
@@ -446,13 +468,25 @@ int mx_batch_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t*
     const uint64_t split = ((uint64_t)a.steps * batch + 7) / 8;
     if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
     if (launch_pdl(mx_batch_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
-    // A thread block per SM, or, where that uses five sixths of them at least, so many that each has part of one tile only.
-    const uint64_t sms = (uint64_t)ctx->sm_count, apart = a.tiles <= sms ? sms / a.tiles * a.tiles : 0;
-    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles * a.steps, apart * 6 >= sms * 5 ? apart : sms);
-    // as many stages as shared memory holds
-    if (a.npad <= 48) return launch_batch<9>(ctx, a, grid, st);
-    if (a.npad <= 96) return launch_batch<7>(ctx, a, grid, st);
-    return launch_batch<5>(ctx, a, grid, st);
+    // A thread block per SM.  Few tiles: as many blocks per tile as take least, at 0.4 us a step and 0.3 us per block, and 16 rows of X, for adding up
+    // (4096 x 4096, 20 rows: 9 blocks per tile 18.5 us, 4 of them 14.8 us).
+    const uint64_t sms = (uint64_t)ctx->sm_count;
+    uint64_t blocks = sms;
+    if (a.tiles * 2ull <= sms) {
+        uint64_t best = ~0ull;
+        for (uint64_t s = 1; s <= std::min<uint64_t>(sms / a.tiles, a.steps); ++s) {
+            const uint64_t cost = (a.steps + s - 1) / s * 4 + (s > 1 ? 3 * s * ((uint64_t)(batch + 15) / 16) : 0);
+            if (cost < best) { best = cost; blocks = s * a.tiles; }
+        }
+    }
+    const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles * a.steps, blocks);
+    a.stages = a.npad <= 96 ? 3u : 2u;
+    const size_t smem = 1024 + (size_t)a.stages * (kBatchA + 1024u) + kBatchPacked * kBatchCode + kRawScales * kBatchRows * 16 + (size_t)kBatchX * batch_x_bytes(a.npad);
+    CUtensorMap code_map, scale_map;
+    if (!make_byte_map(ctx->device, a.codes, a.code_pitch, a.n_out, kBatchCols / 2, kBatchRows, false, &code_map) ||
+        !make_byte_map(ctx->device, a.scales, a.scale_pitch, a.n_out, 16, kBatchRows, false, &scale_map)) return LLVQ_ECUDA;
+    if (!set_smem<mx_batch_kernel>(ctx, smem)) return LLVQ_ECUDA;
+    return launch_pdl(mx_batch_kernel, grid, kBatchThreads, smem, st, code_map, scale_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 }  // namespace llvq
