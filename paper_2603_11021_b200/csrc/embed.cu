@@ -37,14 +37,14 @@ __device__ __forceinline__ int64_t load_token(const void* tokens, int bytes, int
 
 __device__ __forceinline__ uint32_t shift_words(uint32_t a, uint32_t b, uint32_t bytes) { return __funnelshift_r(a, b, bytes * 8u); }
 
-// The 16 bytes at p (any multiple of 2 bytes), all of them inside [begin, end).
-__device__ __forceinline__ uint4 load16(const uint8_t* p, const uint8_t* begin, const uint8_t* end)
+// The 16 bytes at p (any multiple of 2 bytes).  around: the aligned 32 bytes that hold them may be read.
+__device__ __forceinline__ uint4 load16(const uint8_t* p, bool around)
 {
     const uint32_t k = (uint32_t)reinterpret_cast<uintptr_t>(p) & 15u;
     if (k == 0u) return __ldg(reinterpret_cast<const uint4*>(p));
-    const uint8_t* lo = p - k;
-    if (lo >= begin && lo + 32 <= end) {
-        const uint4 a = __ldg(reinterpret_cast<const uint4*>(lo)), b = __ldg(reinterpret_cast<const uint4*>(lo) + 1);
+    if (around) {
+        const uint4* lo = reinterpret_cast<const uint4*>(p - k);
+        const uint4 a = __ldg(lo), b = __ldg(lo + 1);
         uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         if (k & 8u) {
 #pragma unroll
@@ -82,6 +82,14 @@ __device__ __forceinline__ uint4 mx_row8(const uint8_t* codes, const uint8_t* sc
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = v[j] * (j < (int)left ? f0 : f1) * scale;      // the first product is exact
     return make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+}
+
+// Element c alone.
+__device__ __forceinline__ __nv_bfloat16 mx_element(const uint8_t* codes, const uint8_t* scales, uint32_t c, float scale)
+{
+    float v[8];
+    mx_expand8((uint32_t)__ldg(codes + (c >> 1)) >> (4u * (c & 1u)) & 15u, v);
+    return __float2bfloat16_rn(v[0] * mx_scale_value(__ldg(scales + (c >> 5))) * scale);
 }
 
 // Two products with one factor.
@@ -168,40 +176,41 @@ rows_kernel(Rows a)
 #pragma unroll
                 for (int u = 0; u < kRowUnits; ++u) val[u] = mx_word8(w[u], e[u], a.scale, true);
             }
-            uint32_t at[kRowUnits], len[kRowUnits];
+            // pieces that are whole; the elements ahead of the first boundary and behind the last one by a lane each
+            const uint32_t whole = dim > head ? (dim - head) / E : 0u, from_here = kEven && kMx ? 0u : head;
+            const bool inside = from >= a.src + 16 && from + a.src_pitch + 16 <= a.src_end;      // also what lies 16 bytes around the row is in the table
+            if constexpr (!(kMx && kEven)) {
 #pragma unroll
-            for (int u = 0; u < kRowUnits; ++u) {
-                const uint32_t q = q0 + u * lanes;
-                at[u] = head == 0u ? q * E : q == 0u ? 0u : head + (q - 1u) * E;
-                len[u] = q < a.units && at[u] < dim ? min(!kEven && head != 0u && q == 0u ? head : (uint32_t)E, dim - at[u]) : 0u;
-                if constexpr (!(kMx && kEven)) {
-                    val[u] = make_uint4(0u, 0u, 0u, 0u);
-                    if (len[u] == 0u || !known) continue;
-                    if constexpr (kMx) val[u] = mx_row8(from, scales, kb, at[u], a.scale);
+                for (int u = 0; u < kRowUnits; ++u) {
+                    const uint32_t q = min(q0 + u * lanes, whole - 1u), at = from_here + q * E;
+                    if (whole == 0u) continue;
+                    if constexpr (kMx) val[u] = mx_row8(from, scales, kb, at, a.scale);
                     else {
-                        const T* p = reinterpret_cast<const T*>(from) + at[u];
-                        if (len[u] == (uint32_t)E) val[u] = load16(reinterpret_cast<const uint8_t*>(p), a.src, a.src_end);
-                        else {
-                            T* v = reinterpret_cast<T*>(&val[u]);
-#pragma unroll
-                            for (int j = 0; j < E; ++j)
-                                if (j < (int)len[u]) v[j] = p[j];
-                        }
+                        const T* p = reinterpret_cast<const T*>(from) + at;
+                        val[u] = load16(reinterpret_cast<const uint8_t*>(p), inside);
                     }
                 }
             }
 #pragma unroll
             for (int u = 0; u < kRowUnits; ++u) {
-                T* v = reinterpret_cast<T*>(&val[u]);
+                const uint32_t q = q0 + u * lanes;
                 if (!kMx && a.scale != 1.0f) {
+                    T* v = reinterpret_cast<T*>(&val[u]);
 #pragma unroll
                     for (int j = 0; j < E; ++j) v[j] = scaled(v[j], a.scale);
                 }
-                if (len[u] == (uint32_t)E) *reinterpret_cast<uint4*>(out + at[u]) = val[u];
-                else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j)
-                        if (j < (int)len[u]) out[at[u] + j] = v[j];
+                if (q < whole) *reinterpret_cast<uint4*>(out + from_here + q * E) = known ? val[u] : make_uint4(0u, 0u, 0u, 0u);
+            }
+            if (part == 0) {
+                const uint32_t tail = from_here + whole * E, edges = dim > head ? head + (dim - tail) : dim;
+                for (uint32_t i = in; i < edges; i += lanes) {
+                    const uint32_t c = dim > head && (int)i >= (int)head ? tail + (i - head) : i;
+                    T v = T(0.0f);
+                    if (known) {
+                        if constexpr (kMx) v = mx_element(from, scales, c, a.scale);
+                        else v = a.scale != 1.0f ? scaled(reinterpret_cast<const T*>(from)[c], a.scale) : reinterpret_cast<const T*>(from)[c];
+                    }
+                    out[c] = v;
                 }
             }
         }
@@ -236,10 +245,12 @@ int launch_rows(Rows a, cudaStream_t st)
 // grad[v] = scale * sum of dy[i] over the i with token v, in an order that the inputs alone fix: the positions are sorted by token
 // (stably), pieces of kPiece sorted positions are summed one position after the other in binary32, and the sums of a token whose positions
 // lie in several pieces are added in the order of the pieces.  No floating-point atomics.
-// Four kernels: one cluster of thread blocks sorts (a single block, without the cluster's barriers, up to 4096 tokens) while the next kernel
-// clears all rows; then the sums, then those of them that reach across pieces.
+// Four kernels: the sort (up to kRankTokens tokens every token's place by comparison with all others, on all SMs; beyond, digit by digit in one
+// cluster of thread blocks) while the next kernel clears all rows; then the sums, then those of them that reach across pieces.
 // Bound by HBM: dy is read and the gradient written once, and the rows that tokens name are written a second time.
-constexpr int kSortWarps = 32, kSortBits = 9, kSortBins = 1 << kSortBits;
+constexpr int kSortCtas = 8, kSortWarps = 32, kSortBits = 9, kSortBins = 1 << kSortBits;
+// Gradients of 20000 x 256: 2048 tokens 15.0 us by comparison, 8192 tokens 35.8 us by comparison and 24.5 us by digits, 2049 tokens by digits 18.8 us.
+constexpr int kRankTokens = 2048, kRankWarps = 8;
 constexpr int kClearBytes = 64 << 10;   // per thread block: many short ones write faster than a few that stay (2.1 GB: 300 us against 340)
 constexpr int kSpan = 256;              // columns per warp of the sums: eight per lane
 constexpr int kSumWarps = 8;
@@ -260,26 +271,78 @@ struct EmbedGrad {
     unsigned long long* bad_index;
 };
 
+// What a token is sorted by: vocab, behind all others, where it has no row.
+__device__ __forceinline__ uint32_t key_of(const EmbedGrad& a, int64_t token)
+{
+    return token < 0 || token >= a.vocab || token == a.padding ? (uint32_t)a.vocab : (uint32_t)token;
+}
+
+// Up to kRankTokens tokens: the place of each is the number of smaller keys and of equal ones ahead of it.  A thread block places 32 tokens, one per
+// lane, and its warps share the others, all of which it holds in shared memory (rounded up to whole groups with keys that are larger than all).
+__global__ void __launch_bounds__(kRankWarps * 32)
+embed_rank_kernel(EmbedGrad a)
+{
+    extern __shared__ __align__(16) uint32_t rank_keys[];
+    __shared__ uint32_t places[kRankWarps][32];
+    pdl_wait();
+    pdl_launch_dependents();                             // behind the wait: the clearing kernel does not wait, and may write what an earlier kernel read
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t n = (uint32_t)a.n, groups = (n + 31u) / 32u;
+    constexpr int kAhead = 8;                            // tokens that a thread has requested
+    for (uint32_t i0 = threadIdx.x; i0 < groups * 32u; i0 += kAhead * kRankWarps * 32) {
+        int64_t token[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) token[u] = load_token(a.tokens, a.token_bytes, min(i0 + u * (kRankWarps * 32u), n - 1u));
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t i = i0 + u * (kRankWarps * 32u), k = key_of(a, token[u]);
+            if (i < n && k == (uint32_t)a.vocab && token[u] != a.padding && i / 32u == blockIdx.x) atomicAdd(a.bad_index, 1ull);
+            if (i < groups * 32u) rank_keys[i] = i < n ? k : 0xffffffffu;
+        }
+    }
+    __syncthreads();
+    const uint32_t mine = rank_keys[blockIdx.x * 32u + lane];
+    uint32_t place = 0;
+    for (uint32_t g = warp; g < groups; g += kRankWarps) {
+        const uint4* k = reinterpret_cast<const uint4*>(rank_keys + g * 32u);
+        if (g == blockIdx.x) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) { const uint32_t other = rank_keys[g * 32u + j]; place += other < mine || (other == mine && j < lane) ? 1u : 0u; }
+        } else {
+            const uint32_t border = mine + (g < blockIdx.x ? 1u : 0u);      // equal keys ahead count; keys are below 2^31
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint4 v = k[j];
+                place += (v.x < border ? 1u : 0u) + (v.y < border ? 1u : 0u) + (v.z < border ? 1u : 0u) + (v.w < border ? 1u : 0u);
+            }
+        }
+    }
+    places[warp][lane] = place;
+    __syncthreads();
+    const uint32_t i = blockIdx.x * 32u + lane;
+    if (warp == 0 && i < n) {
+#pragma unroll
+        for (int w = 1; w < kRankWarps; ++w) place += places[w][lane];
+        a.key[a.sorted][place] = mine;
+        a.pos[a.sorted][place] = i;
+    }
+}
+
 // One digit.  A warp takes a contiguous run of items, 32 at a time, in both loops; place of an item = items of smaller digits + of the same
 // digit in earlier thread blocks, warps and steps + in lower lanes.
-template <int kSortCtas>
 __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_t* total, uint32_t* base, uint32_t* warp_sum)
 {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, bins = 1 << a.bits, shift = pass * a.bits;
-    const uint32_t rank = kSortCtas > 1 ? cluster.block_rank() : 0u;
+    const uint32_t rank = cluster.block_rank();
     const int64_t runs = kSortCtas * kSortWarps, run = (a.n + runs * 32 - 1) / (runs * 32) * 32;
     const int64_t begin = min((rank * kSortWarps + warp) * run, a.n), end = min(begin + run, a.n);
     const uint32_t *key = a.key[pass & 1], *pos = a.pos[pass & 1];
     uint32_t *key_out = a.key[(pass & 1) ^ 1], *pos_out = a.pos[(pass & 1) ^ 1];
     uint32_t* mine = hist + warp * kSortBins;
     const uint32_t below = (1u << lane) - 1u;
-    auto item = [&](int64_t i) -> uint32_t {
-        if (pass > 0) return key[i];
-        const int64_t v = load_token(a.tokens, a.token_bytes, i);
-        return v < 0 || v >= a.vocab || v == a.padding ? (uint32_t)a.vocab : (uint32_t)v;
-    };
+    auto item = [&](int64_t i) -> uint32_t { return pass > 0 ? key[i] : key_of(a, load_token(a.tokens, a.token_bytes, i)); };
     for (int b = lane; b < bins; b += 32) mine[b] = 0u;
     __syncwarp();
     for (int64_t i = begin; i < end; i += 32) {
@@ -297,10 +360,9 @@ __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_
         for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = hist[w * kSortBins + tid]; hist[w * kSortBins + tid] = sum; sum += c; }
         total[tid] = sum;
     }
-    if (kSortCtas > 1) cluster.sync();
+    cluster.sync();
     uint32_t before = 0, all = 0;
-    if (kSortCtas == 1 && tid < bins) all = total[tid];
-    if (kSortCtas > 1 && tid < bins) {
+    if (tid < bins) {
         for (int c = 0; c < kSortCtas; ++c) {
             const uint32_t v = *cluster.map_shared_rank(total + tid, c);
             if (c < (int)rank) before += v;
@@ -334,11 +396,9 @@ __device__ void sort_digit(const EmbedGrad& a, int pass, uint32_t* hist, uint32_
             pos_out[at] = pass > 0 ? pos[i + lane] : (uint32_t)(i + lane);
         }
     }
-    if (kSortCtas > 1) cluster.sync();                   // the next digit, and its counters, after all of this one; what was written is seen
-    else __syncthreads();
+    cluster.sync();                                      // the next digit, and its counters, after all of this one; what was written is seen
 }
 
-template <int kSortCtas>
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortWarps * 32, 1)
 embed_sort_kernel(EmbedGrad a)
 {
@@ -347,7 +407,7 @@ embed_sort_kernel(EmbedGrad a)
     pdl_launch_dependents();                             // behind the wait: the clearing kernel does not wait, and may write what an earlier kernel read
     uint32_t* hist = sort_smem;
     uint32_t *total = hist + kSortWarps * kSortBins, *base = total + kSortBins, *warp_sum = base + kSortBins;
-    for (int pass = 0; pass < a.passes; ++pass) sort_digit<kSortCtas>(a, pass, hist, total, base, warp_sum);
+    for (int pass = 0; pass < a.passes; ++pass) sort_digit(a, pass, hist, total, base, warp_sum);
 }
 
 // Clears [p, p + bytes) while the sort is running.  Its last thread block ends after the sort has: what waits for this kernel finds both done.
@@ -507,11 +567,14 @@ embed_join_kernel(EmbedGrad a, int64_t pieces, uint32_t spans)
     const uint32_t key = keys[last];
     if (key == (uint32_t)a.vocab || keys[last + 1] != key) return;                        // nothing reaches out of the piece
     if (piece > 0 && keys[piece * a.piece] == key && keys[piece * a.piece - 1] == key) return;   // it began in an earlier one
-    int64_t lo = piece + 1, hi = pieces;                // first piece that does not begin with the token
+    int64_t lo = piece + 1, hi = pieces;                // the first piece that does not begin with the token is in [lo, hi]: 32 of them looked at together
     while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
-        if (keys[mid * a.piece] == key) lo = mid + 1;
-        else hi = mid;
+        const int64_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t same = __ballot_sync(0xffffffffu, at < hi && keys[at * a.piece] == key);
+        const int t = __popc(same);                      // the first t of them do
+        const int64_t end = lo + t * step;
+        if (t > 0) lo = end - step + 1;
+        hi = min(hi, end);
     }
     const int64_t more = lo - (piece + 1), run = (more + kSumWarps - 1) / kSumWarps;
     float sum[8] = {};
@@ -678,8 +741,10 @@ int llvq_embed_grad(const llvq_ctx* ctx, const void* d_dy, int dy_dtype, const v
     const uint32_t spans = (uint32_t)((dim + kSpan - 1) / kSpan);
     if (clearing > 0x7fffffff || pieces * (int64_t)spans > 0x7fffffff) return LLVQ_EUNSUPPORTED;
     const size_t smem = (size_t)(kSortWarps * kSortBins + 2 * kSortBins + kSortWarps) * 4;
-    if (!set_smem<embed_sort_kernel<1>>(ctx, smem) || !set_smem<embed_sort_kernel<8>>(ctx, smem)) return LLVQ_ECUDA;
-    const cudaError_t r = n <= 4096 ? launch_pdl(embed_sort_kernel<1>, 1u, kSortWarps * 32, smem, st, a) : launch_pdl(embed_sort_kernel<8>, 8u, kSortWarps * 32, smem, st, a);
+    if (!set_smem<embed_sort_kernel>(ctx, smem)) return LLVQ_ECUDA;
+    const unsigned groups = (unsigned)((n + 31) / 32);
+    const cudaError_t r = n <= kRankTokens ? launch_pdl(embed_rank_kernel, groups, kRankWarps * 32, groups * 128, st, a)
+                                           : launch_pdl(embed_sort_kernel, (unsigned)kSortCtas, kSortWarps * 32, smem, st, a);
     if (r != cudaSuccess) return LLVQ_ECUDA;
     if (!accumulate && launch_pdl(embed_clear_kernel, (unsigned)clearing, 1024, 0, st, static_cast<uint8_t*>(d_grad), clear) != cudaSuccess) return LLVQ_ECUDA;
     return dy_dtype == LLVQ_F32    ? launch_sums<float>(a, grad_dtype, pieces, spans, st)
