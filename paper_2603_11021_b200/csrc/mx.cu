@@ -516,39 +516,51 @@ int mx_stream_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t
     a.x = reinterpret_cast<const __nv_bfloat16*>(d_x); a.batch = batch; a.y = d_y; a.flags = ctx->dev.flags; a.x_chunks = work;
     a.x_align = 8;
     while (a.x_align > 1 && (!aligned(d_x, 2 * (size_t)a.x_align) || (batch > 1 && k_in % a.x_align != 0))) a.x_align /= 2;
-    constexpr int kWarps = 16;
     const int tiles = (batch + 7) / 8;
-    constexpr uint32_t fixed = Stream<kWarps, true>::kCodes + Stream<kWarps, true>::kScales;
-    // Rows of a tile: what takes the fewest rounds over the SMs, counted in rows, with a quarter of the smallest tile on top for the end of a tile,
-    // no more warps along a row than it has chunks, and two stages at least.
+    // Warps and rows of a tile by what they should take, in ns: the rounds over the SMs, each with the tile's share of W (17 bytes per block) and, half as
+    // dear, of X at 35 bytes per ns, and an end; with two stages at least and no more warps along a row than it has chunks.  16 warps take
+    // 0.7 us longer to start; eight are slower at the products (28672 x 8192, us with 16 / 8: one row 32.0 / 39.2, eight 31.0 / 32.2, 16 rows 40.8 / 47.4)
+    // and make room for stages (8192 x 8192, 16 rows: 22.9 / 16.0; 2048 x 4096, one row 4.2 / 3.5, 16 rows 13.0 / 6.2).
+    const int slower = batch == 1 ? 123 : batch <= 8 ? 103 : 116;      // per cent
     uint64_t best = ~0ull;
     size_t smem = 0;
-    for (int l = 4; l >= 0; --l) {
-        const int kg = kWarps >> l;
-        if (l < 4 && kg / 2 >= (int)a.chunks) break;
-        const uint32_t stage = (fixed + (uint32_t)(kg * batch) * kXPitch + 1023u) & ~1023u;
-        const uint32_t part = kg > 1 ? (uint32_t)kg * tiles * 8u * (16u << l) * 4u : 0u;
-        const int stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / stage);
-        if (stages < 2) continue;
-        const uint64_t count = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), cost = (count + ctx->sm_count - 1) / ctx->sm_count * ((4u << l) + 1u);
-        if (cost >= best) continue;
-        best = cost;
-        a.rg_log2 = l; a.tiles = (uint32_t)count; a.stage_bytes = stage; a.stages = stages; a.part_at = (uint32_t)stages * stage;
-        smem = 1024 + a.part_at + part;
+    int warps = 0;
+    for (int w = 16; w >= 8; w /= 2) {
+        for (int l = w == 16 ? 4 : 3; l >= 0; --l) {
+            const int kg = w >> l;
+            if (kg > 1 && kg / 2 >= (int)a.chunks) break;
+            const uint32_t stage = ((uint32_t)w * (16u * (kChunk / 2) + 16u * 16u) + (uint32_t)(kg * batch) * kXPitch + 1023u) & ~1023u;
+            const uint32_t part = kg > 1 ? (uint32_t)kg * tiles * 8u * (16u << l) * 4u : 0u;
+            const int stages = (int)std::min<size_t>(6, (kStreamSmem - 1024 - part) / stage);
+            if (stages < 2) continue;
+            const uint64_t count = ((uint64_t)n_out + (16u << l) - 1) / (16u << l), rounds = (count + ctx->sm_count - 1) / ctx->sm_count;
+            const uint64_t bytes = (uint64_t)a.kb * ((16u << l) * 17u + (uint64_t)batch * 34u);
+            const uint64_t cost = rounds * (bytes / 35u + 100u) * (w == 8 ? slower : 100) / 100u + (w == 16 ? 700u : 0u);
+            if (cost >= best) continue;
+            best = cost;
+            warps = w;
+            a.rg_log2 = l; a.tiles = (uint32_t)count; a.stage_bytes = stage; a.stages = stages; a.part_at = (uint32_t)stages * stage;
+            smem = 1024 + a.part_at + part;
+        }
     }
     if (best == ~0ull) return LLVQ_EUNSUPPORTED;
     CUtensorMap codes, scales;
     if (!make_byte_map(ctx->device, d_codes, mx_code_pitch(k_in), n_out, 128, 16 << a.rg_log2, true, &codes) ||
         !make_byte_map(ctx->device, d_scales, mx_scale_pitch(k_in), n_out, 16, 16 << a.rg_log2, false, &scales)) return LLVQ_ECUDA;
     const unsigned grid = std::min<unsigned>(a.tiles, (unsigned)ctx->sm_count);
-    if (batch == 1)
-        return y_dtype == LLVQ_F32 ? launch_stream<kWarps, 1, true, false>(ctx, codes, scales, a, grid, smem, st)
-                                   : launch_stream<kWarps, 1, false, false>(ctx, codes, scales, a, grid, smem, st);
-    const uint64_t split = ((uint64_t)a.chunks * batch + 7) / 8;
-    if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
-    if (launch_pdl(mx_stream_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
-    return tiles == 1 ? launch_stream<kWarps, 1, false, true>(ctx, codes, scales, a, grid, smem, st)
-                      : launch_stream<kWarps, 2, false, true>(ctx, codes, scales, a, grid, smem, st);
+    if (batch > 1) {
+        const uint64_t split = ((uint64_t)a.chunks * batch + 7) / 8;
+        if (split > 0x7fffffff) return LLVQ_EUNSUPPORTED;
+        if (launch_pdl(mx_stream_split_kernel, (unsigned)split, 256, 0, st, a) != cudaSuccess) return LLVQ_ECUDA;
+    }
+    auto launch = [&](auto w) {
+        constexpr int kWarps = decltype(w)::value;
+        return batch == 1 ? y_dtype == LLVQ_F32 ? launch_stream<kWarps, 1, true, false>(ctx, codes, scales, a, grid, smem, st)
+                                                : launch_stream<kWarps, 1, false, false>(ctx, codes, scales, a, grid, smem, st)
+               : tiles == 1 ? launch_stream<kWarps, 1, false, true>(ctx, codes, scales, a, grid, smem, st)
+                            : launch_stream<kWarps, 2, false, true>(ctx, codes, scales, a, grid, smem, st);
+    };
+    return warps == 16 ? launch(std::integral_constant<int, 16>{}) : launch(std::integral_constant<int, 8>{});
 }
 
 }  // namespace
