@@ -114,10 +114,12 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, uint32_t cols, int64_t
 // leaves every bf16 number exact down to 2^-32 of that magnitude and puts smaller ones off by at most 2^-40 of it, far below the rounding of
 // the sums (binary32, 2^-24 of the same magnitude).
 //
-// A thread block streams W: warp 8 copies the codes of RG x 16 rows and KG x 512 columns per stage with TMA (rows of 128 bytes, swizzled, so that
-// ldmatrix reads 16 bytes of eight rows without conflicts and hands each lane the word of codes whose elements are its own in the tile) and their
-// scales; warps 9 to 12 bring the same columns of X; warps 0 to 7 multiply, 16 rows by 512 columns each, RG x KG = 8 (up to 16 rows of X: 16 warps).  The stages in flight are
-// what hides the latency of HBM, which bounds the kernel up to about 24 rows of X (4.25 bits per weight, read once); beyond, the products do.
+// A thread block streams W: kWarps warps multiply, 16 rows by 512 columns each per stage, RG x 16 rows by KG x 512 columns together, RG x KG = kWarps.
+// The next warp copies their codes with TMA (rows of 128 bytes, swizzled, so that ldmatrix reads 16 bytes of eight rows without conflicts and hands each
+// lane the word of codes whose elements are its own in the tile) and their scales.  X: one row is brought and converted by four more warps;
+// several rows are converted once ahead by a kernel of their own and copied by one more warp, and W is read while that kernel still runs.  The stages in
+// flight are what hides the latency of HBM, which bounds the kernel for up to about 16 rows of X (4.25 bits per weight, read once: 128256 x 4096,
+// one row, 54 us, 79 % of the measured bandwidth); beyond, the products do.
 constexpr int kChunk = 512;                              // columns of a warp's part of a stage
 constexpr int kXWarps = 4;
 constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice; the exponent is behind the columns
@@ -503,11 +505,13 @@ int launch_stream(const llvq_ctx* ctx, const CUtensorMap& codes, const CUtensorM
     return r == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
-constexpr int kStreamBatch = 16;                         // rows of X up to which weights go through registers; beyond, mx_batch_product
+// Whether weights go through registers (mx_stream_kernel) or to the tensor cores as they are (mx_batch_product).  us: 4096 x 4096, 17 / 24 / 32 rows of X
+// 11.0 / 11.3 / 14.1 and 14.5 / 15.5 / 16.0; 11008 x 4096 17.3 / 17.4 / 22.6 and 16.2 / 16.8 / 17.7; 28672 x 8192, 17 rows 63 and 38.
+bool takes_stream(int64_t n_out, int64_t k_in, int batch) { return batch <= 16 || (batch <= 32 && n_out <= (1ll << 25) / k_in); }
 
 uint64_t stream_x_bytes(int64_t k_in, int batch) { return (uint64_t)(k_in + kChunk - 1) / kChunk * (uint64_t)batch * kXPitch; }
 
-// batch up to kStreamBatch; work: stream_x_bytes() of device memory for more than one row
+// batch up to 32; work: stream_x_bytes() of device memory for more than one row
 int mx_stream_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x, int batch,
                       void* d_y, int y_dtype, uint8_t* work, cudaStream_t st)
 {
@@ -525,7 +529,7 @@ int mx_stream_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t
     uint64_t best = ~0ull;
     size_t smem = 0;
     int warps = 0;
-    for (int w = 16; w >= 8; w /= 2) {
+    for (int w = tiles <= 2 ? 16 : 8; w >= 8; w /= 2) {
         for (int l = w == 16 ? 4 : 3; l >= 0; --l) {
             const int kg = w >> l;
             if (kg > 1 && kg / 2 >= (int)a.chunks) break;
@@ -560,6 +564,8 @@ int mx_stream_product(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t
                : tiles == 1 ? launch_stream<kWarps, 1, false, true>(ctx, codes, scales, a, grid, smem, st)
                             : launch_stream<kWarps, 2, false, true>(ctx, codes, scales, a, grid, smem, st);
     };
+    if (tiles == 3) return launch_stream<8, 3, false, true>(ctx, codes, scales, a, grid, smem, st);
+    if (tiles == 4) return launch_stream<8, 4, false, true>(ctx, codes, scales, a, grid, smem, st);
     return warps == 16 ? launch(std::integral_constant<int, 16>{}) : launch(std::integral_constant<int, 8>{});
 }
 
@@ -605,7 +611,7 @@ int llvq_mx_gemv(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_s
 size_t llvq_mx_small_batch_bytes(const llvq_ctx* ctx, int64_t n_out, int64_t k_in, int batch)
 {
     if (!ctx || ctx->device < 0 || n_out <= 0 || k_in <= 0 || batch <= 0 || batch > 64 || n_out > (1ll << 30) || k_in > (1ll << 30)) return 0;
-    return batch == 1 ? 0 : batch <= kStreamBatch ? (size_t)stream_x_bytes(k_in, batch) : mx_batch_bytes(ctx, n_out, k_in, batch);
+    return batch == 1 ? 0 : takes_stream(n_out, k_in, batch) ? (size_t)stream_x_bytes(k_in, batch) : mx_batch_bytes(ctx, n_out, k_in, batch);
 }
 
 int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_scales, int64_t n_out, int64_t k_in, const uint16_t* d_x_bf16,
@@ -622,7 +628,7 @@ int llvq_mx_gemm_small_batch(const llvq_ctx* ctx, const uint8_t* d_codes, const 
     cudaStream_t st = (cudaStream_t)stream;
     if (k_in == 0) return cudaMemsetAsync(d_y_bf16, 0, (size_t)n_out * batch * 2, st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
     uint8_t* work = static_cast<uint8_t*>(d_work);
-    return batch <= kStreamBatch ? mx_stream_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, LLVQ_BF16, work, st)
+    return takes_stream(n_out, k_in, batch) ? mx_stream_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, LLVQ_BF16, work, st)
                                  : mx_batch_product(ctx, d_codes, d_scales, n_out, k_in, d_x_bf16, batch, d_y_bf16, work, st);
 }
 

@@ -112,17 +112,54 @@ def test_small_batches(P, ctx, batch, n_out, k_in):
     check_product(y, f64(x), mx.values_of(codes, scales, k_in))
 
 
+@pytest.mark.parametrize("batch", [1, 5, 17, 32, 33, 64])
+@pytest.mark.parametrize("n_out,k_in", [(9000, 3850), (300, 12000), (2600, 13000)])
+def test_larger_matrices(P, ctx, batch, n_out, k_in):
+    # sizes at which thread blocks share tiles, take several of them, and change from one form of the product to the other
+    codes, scales = mx.random_matrix(n_out, k_in, seed=n_out)
+    x = torch.randn((batch, k_in), generator=torch.Generator().manual_seed(batch)).bfloat16()
+    y = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), n_out, k_in, x.cuda())
+    check_product(y, f64(x), mx.values_of(codes, scales, k_in))
+
+
+@pytest.mark.parametrize("batch", [1, 3, 20, 40])
+def test_an_infinity_in_the_activations(P, ctx, batch):
+    # +-inf where the weight is not zero, NaN where it is, as products in binary32 give; other rows as if it were not there
+    codes, scales = mx.random_matrix(300, 480, seed=3)
+    w = mx.values_of(codes, scales, 480)
+    x = torch.randn((batch, 480), generator=torch.Generator().manual_seed(1)).bfloat16()
+    clean = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 300, 480, x.cuda())
+    x[0, 77] = float("inf")
+    y = f64(P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 300, 480, x.cuda()))
+    want = np.where(w[:, 77] == 0, np.nan, np.sign(w[:, 77]) * np.inf)
+    assert np.array_equal(y[0], want, equal_nan=True) and np.array_equal(y[1:], f64(clean)[1:])
+
+
+@pytest.mark.parametrize("batch", [1, 3, 20, 40])
+def test_activations_of_very_different_sizes(P, ctx, batch):
+    # one channel 2^17 times the others, where every weight is zero: the others count as if it were not there (down to 2^-19 of the largest exactly)
+    codes, scales = mx.random_matrix(64, 480, seed=3)
+    codes[:, 50] = 0                                          # columns 100 and 101
+    x = torch.randn((batch, 480), generator=torch.Generator().manual_seed(1)).bfloat16()
+    x[:, 100] = 2.0 ** 17
+    x[:, 101] = 0
+    x = torch.where(x.abs() < 2.0 ** -2, torch.zeros_like(x), x)
+    y = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 64, 480, x.cuda())
+    check_product(y, f64(x), mx.values_of(codes, scales, 480))
+
+
 @pytest.mark.parametrize("lo,hi", [(0, 3), (126, 130), (120, 200), (8, 240)])
 def test_products_over_the_whole_range_of_scales(P, ctx, lo, hi):
     # activations that bring the products back into the middle of binary32's range
     n_out, k_in = 32, 1024
     codes, scales = mx.random_matrix(n_out, k_in, seed=lo, lo=lo, hi=hi)
     w = mx.values_of(codes, scales, k_in)
-    x = torch.randn((3, k_in), generator=torch.Generator().manual_seed(1)) * 2.0 ** (122 - (lo + hi) // 2)
+    x = torch.randn((40, k_in), generator=torch.Generator().manual_seed(1)) * 2.0 ** (122 - (lo + hi) // 2)
     x = x.bfloat16()
     y = P.llvq_mx_gemv(ctx, dev(codes), dev(scales), n_out, k_in, x[0].cuda())
     check_product(y[None], f64(x[:1]), w)
-    check_product(P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), n_out, k_in, x.cuda()), f64(x), w)
+    for batch in (3, 20, 40):
+        check_product(P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), n_out, k_in, x[:batch].cuda()), f64(x[:batch]), w)
 
 
 def test_a_block_that_is_nan_reaches_its_row_alone(P, ctx):
@@ -132,6 +169,8 @@ def test_a_block_that_is_nan_reaches_its_row_alone(P, ctx):
     y = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 40, 480, x.cuda())
     check_product(y, f64(x), mx.values_of(codes, scales, 480))
     assert torch.isnan(y[:, 5]).all() and torch.isnan(y).sum() == 3
+    x = torch.randn((50, 480)).bfloat16()
+    check_product(P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 40, 480, x.cuda()), f64(x), mx.values_of(codes, scales, 480))
 
 
 def test_activations_that_are_not_finite_reach_their_own_row(P, ctx):
@@ -154,12 +193,13 @@ def test_activations_off_the_16_byte_boundaries(P, ctx, shift):
 
 def test_products_are_the_same_every_time_and_touch_nothing_else(P, ctx):
     codes, scales = (dev(a) for a in mx.random_matrix(1000, 4096, seed=3))
-    x = torch.randn((20, 4096), device="cuda").bfloat16()
-    y = torch.full((20 * 1000 + 8,), 3.0, dtype=torch.bfloat16, device="cuda")
-    P.llvq_mx_gemm_small_batch(ctx, codes, scales, 1000, 4096, x, y[4:-4])
-    assert (y[:4] == 3).all() and (y[-4:] == 3).all()
-    for _ in range(3):
-        assert torch.equal(P.llvq_mx_gemm_small_batch(ctx, codes, scales, 1000, 4096, x).view(-1), y[4:-4])
+    for batch in (1, 7, 20, 50):
+        x = torch.randn((batch, 4096), device="cuda").bfloat16()
+        y = torch.full((batch * 1000 + 8,), 3.0, dtype=torch.bfloat16, device="cuda")
+        P.llvq_mx_gemm_small_batch(ctx, codes, scales, 1000, 4096, x, y[4:-4])
+        assert (y[:4] == 3).all() and (y[-4:] == 3).all()
+        for _ in range(3):
+            assert torch.equal(P.llvq_mx_gemm_small_batch(ctx, codes, scales, 1000, 4096, x).view(-1), y[4:-4])
 
 
 def test_nothing_to_do(P, ctx):
@@ -183,8 +223,9 @@ def test_misaligned_codes_are_refused(P, ctx):
         assert e.value.status == 2
 
 
-def test_captured_and_on_another_stream(P, ctx):
-    x = torch.randn((16, 1024), device="cuda").bfloat16()
+@pytest.mark.parametrize("batch", [16, 50])
+def test_captured_and_on_another_stream(P, ctx, batch):
+    x = torch.randn((batch, 1024), device="cuda").bfloat16()
     w = torch.randn((512, 1024), device="cuda")
     wc, ws = P.llvq_mx_quantize(ctx, w)
     y = P.llvq_mx_gemm_small_batch(ctx, wc, ws, 512, 1024, x)
