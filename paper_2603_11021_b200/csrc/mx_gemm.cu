@@ -8,35 +8,39 @@ namespace {
 using namespace llvq;
 
 // tcgen05.mma.kind::mxf4 takes e2m1 operands from shared memory and one e8m0 scale per row and 32 columns from tensor memory: nothing of
-// either operand passes through registers.  A thread block computes tiles of 128 rows of W (the lanes of tensor memory) by kBn tokens
-// (its columns), 256 columns of both operands (128 bytes of codes per row) per stage:
-//   warp 0      copies codes with TMA (swizzled rows of 128 bytes; what lies past the matrix reads as zero), and scales, 16 per row at a time
+// either operand passes through registers.  A thread block computes tiles of kRt x 128 rows of W (128 lanes of tensor memory each) by kBn tokens
+// (columns), 256 columns of both operands (128 bytes of codes per row) per stage:
+//   warp 0      copies codes with TMA (swizzled rows of 128 bytes; what lies past the matrix reads as zero)
 //   warps 2, 3  lay the scales of W and X out as tcgen05.cp wants them: of 128 rows and 4 blocks, 512 bytes, row r at 16 (r % 32) + 4 (r / 32).
-//               A lane reads 16 scales of four rows 32 apart (the rows' padding is for that) and stores four times 16 bytes in two stages
-//   warp 1      copies the scales to tensor memory and issues four MMAs of 64 columns per stage
-//   warps 4-11  take the accumulator out as bf16 (a quarter of the lanes by half of the columns each), hand it back, then write Y
-// There is one accumulator: taking it out costs the tensor cores a few hundred of the thousands of cycles of a tile.
+//               A lane copies 16 scales of four rows 32 apart ahead (the rows' padding is for that) and stores four times 16 bytes of them in
+//               two stages.  (With TMA, whose time goes by rows whatever their length, they took as long as half of the codes.)
+//   warp 1      copies the scales to tensor memory and issues four MMAs of 64 columns per 128 rows and stage
+//   warps 4-11  take the accumulators out as bf16, hand them back, then write Y
+// Large products are bound by what TMA and L2 bring, so the large tile is the one that reads least per product: 256 rows by 224 tokens fill tensor
+// memory with two accumulators and two stages' scales (60 KB per stage for 1.75 times the products of 128 x 256, which reads 48 KB).  There is one set
+// of accumulators: taking it out costs the tensor cores a few hundred of the tens of thousands of cycles of a tile.
 constexpr int kMmThreads = 384;
-constexpr int kMmRows = 128;                              // rows of W per tile
 constexpr int kMmGroup = 16;                              // row tiles that are walked together, for L2
 constexpr uint32_t kStageCodes = 128;                     // bytes of a row's codes per stage: 256 columns
 
-template <int kBn> struct MmShape {
-    static constexpr int kBHalves = kBn > 128 ? 2 : 1;    // groups of 128 tokens
-    static constexpr uint32_t kA = kMmRows * kStageCodes, kB = kBn * kStageCodes, kScales = (2 + 2 * kBHalves) * kScaleAtom;
+constexpr int kRawAhead = 3;                              // scales under way, of two stages each
+
+template <int kRt, int kBn> struct MmShape {
+    static constexpr int kRows = 128 * kRt, kBHalves = kBn > 128 ? 2 : 1;      // rows of W; groups of 128 tokens
+    static constexpr uint32_t kA = kRows * kStageCodes, kB = kBn * kStageCodes, kScales = 2 * (kRt + kBHalves) * kScaleAtom;
     static constexpr uint32_t kStage = kA + kB + kScales; // a multiple of 1024
-    static constexpr int kStages = kBn == 256 ? 4 : kBn == 128 ? 6 : 8;
-    static constexpr uint32_t kScaleCols = 8 + 8 * kBHalves;      // columns of tensor memory that a stage's scales take
-    static constexpr uint32_t kTmem = kBn == 256 ? 512 : kBn == 128 ? 256 : 128;
-    static constexpr int kRawEntries = kStages / 2 + 1;   // boxes of scales as they come, of two stages each
-    static constexpr uint32_t kRaw = (kMmRows + kBn) * 16;
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kRawEntries * kRaw + 256;
-    static_assert(kStage % 1024 == 0 && kBn + 2 * kScaleCols <= kTmem && kSmem <= 227 * 1024, "");
+    static constexpr int kStages = kRt == 2 ? 3 : kBn == 256 ? 4 : kBn == 128 ? 6 : 7;
+    static constexpr uint32_t kScaleCols = 8 * (kRt + kBHalves);               // columns of tensor memory that a stage's scales take
+    static constexpr uint32_t kCols = kRt * kBn + 2 * kScaleCols, kTmem = kCols > 256 ? 512 : kCols > 128 ? 256 : 128;
+    static constexpr uint32_t kRaw = (kRt + kBHalves) * 128 * 16;      // scales as they come, of two stages
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kRawAhead * kRaw + 256;
+    static_assert(kStage % 1024 == 0 && kCols <= kTmem && kSmem <= 227 * 1024, "");
 };
 
 struct MmArgs {
+    const uint8_t *w_scales, *x_scales;
     int64_t n_out, tokens;
-    uint32_t kb, k_stages;                                // blocks per row, stages per tile
+    uint32_t kb, pitch, k_stages;                         // blocks per row, bytes per row of scales, stages per tile
     uint32_t tiles_m, tiles_n;
     __nv_bfloat16* y;
     uint32_t* flags;
@@ -78,25 +82,21 @@ __device__ __forceinline__ void mm_tile(const MmArgs& a, uint32_t tile, uint32_t
     m = group * kMmGroup + (in - n * high);
 }
 
-template <int kBn>
+template <int kRt, int kBn>
 __global__ void __launch_bounds__(kMmThreads, 1)
-mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const __grid_constant__ CUtensorMap ws_map,
-               const __grid_constant__ CUtensorMap xs_map, MmArgs a)
+mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, MmArgs a)
 {
-    using S = MmShape<kBn>;
+    using S = MmShape<kRt, kBn>;
     extern __shared__ uint8_t mm_smem[];
     const uint32_t base = (smem_u32(mm_smem) + 1023u) & ~1023u;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(mm_smem + (base - smem_u32(mm_smem)) + S::kStages * S::kStage + S::kRawEntries * S::kRaw);
-    uint64_t *full = bars, *empty = bars + S::kStages, *acc_full = bars + 2 * S::kStages, *acc_empty = acc_full + 1, *raw_full = acc_empty + 1,
-             *raw_empty = raw_full + S::kRawEntries;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(raw_empty + S::kRawEntries);
-    const uint32_t raw = base + S::kStages * S::kStage;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(mm_smem + (base - smem_u32(mm_smem)) + S::kStages * S::kStage + kRawAhead * S::kRaw);
+    uint64_t *full = bars, *empty = bars + S::kStages, *acc_full = bars + 2 * S::kStages, *acc_empty = acc_full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
     const int warp = warp_number(), lane = threadIdx.x & 31;
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) { mbar_init(full + s, 3); mbar_init(empty + s, 1); }      // TMA, scales of W, scales of X
-        for (int e = 0; e < S::kRawEntries; ++e) { mbar_init(raw_full + e, 1); mbar_init(raw_empty + e, 2); }
         mbar_init(acc_full, 1);
         mbar_init(acc_empty, 8);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -112,26 +112,17 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t it = 0, pair = 0;
+            uint32_t it = 0;
             for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
                 uint32_t m, n;
                 mm_tile(a, tile, m, n);
                 for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
-                    if ((k & 1u) == 0u) {
-                        const uint32_t e = pair % S::kRawEntries, turn = pair / S::kRawEntries;
-                        if (turn > 0) ok = mbar_wait(raw_empty + e, (turn - 1u) & 1u);
-                        if (!ok) break;
-                        mbar_expect(raw_full + e, S::kRaw);
-                        tma_load_2d(raw + e * S::kRaw, &ws_map, (int)(k * 8u), (int)(m * kMmRows), raw_full + e);
-                        tma_load_2d(raw + e * S::kRaw + kMmRows * 16u, &xs_map, (int)(k * 8u), (int)(n * kBn), raw_full + e);
-                        ++pair;
-                    }
                     const uint32_t s = it % S::kStages, round = it / S::kStages;
                     if (round > 0) ok = mbar_wait(empty + s, (round - 1u) & 1u);
                     if (!ok) break;
                     const uint32_t at = base + s * S::kStage;
                     mbar_expect(full + s, S::kA + S::kB);
-                    tma_load_2d(at, &w_map, (int)(k * kStageCodes), (int)(m * kMmRows), full + s);
+                    tma_load_2d(at, &w_map, (int)(k * kStageCodes), (int)(m * S::kRows), full + s);
                     tma_load_2d(at + S::kA, &x_map, (int)(k * kStageCodes), (int)(n * kBn), full + s);
                 }
             }
@@ -145,18 +136,22 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t off = s * (S::kStage >> 4), ta = tmem + kBn + buffer * S::kScaleCols, tb = ta + 8;
+                const uint32_t off = s * (S::kStage >> 4), ta = tmem + kRt * kBn + buffer * S::kScaleCols, tb = ta + 8 * kRt;
                 const uint64_t da = da0 + off, db = db0 + off, sc = sc0 + off;
                 if (elect_one()) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        scales_to_tmem(ta + 4 * h, sc + h * (kScaleAtom >> 4));
+                    for (int h = 0; h < 2; ++h) {         // blocks 0-3 and 4-7 of the stage
 #pragma unroll
-                        for (int g = 0; g < S::kBHalves; ++g) scales_to_tmem(tb + h * 4 * S::kBHalves + 4 * g, sc + (2 + g * 2 + h) * (kScaleAtom >> 4));
+                        for (int g = 0; g < kRt; ++g) scales_to_tmem(ta + h * 4 * kRt + 4 * g, sc + (g * 2 + h) * (kScaleAtom >> 4));
+#pragma unroll
+                        for (int g = 0; g < S::kBHalves; ++g) scales_to_tmem(tb + h * 4 * S::kBHalves + 4 * g, sc + (2 * kRt + g * 2 + h) * (kScaleAtom >> 4));
                     }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)           // 64 columns: 32 bytes on along the rows, two blocks on along the scales
-                        umma_mxf4(tmem, da + 2 * q, db + 2 * q, instr_desc_mxf4(kBn, q & 1), ta + 4 * (q >> 1), tb + 4 * S::kBHalves * (q >> 1), k > 0 || q > 0);
+                    for (int g = 0; g < kRt; ++g)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)       // 64 columns: 32 bytes on along the rows, two blocks on along the scales
+                            umma_mxf4(tmem + g * kBn, da + g * (128 * kStageCodes >> 4) + 2 * q, db + 2 * q, instr_desc_mxf4(kBn, q & 1), ta + (q >> 1) * 4 * kRt + 4 * g,
+                                      tb + 4 * S::kBHalves * (q >> 1), k > 0 || q > 0);
                     umma_commit(empty + s);
                 }
                 __syncwarp();
@@ -168,30 +163,58 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         }
     } else if (warp < 4) {
         const bool of_w = warp == 2;
-        const uint32_t from = raw + (of_w ? 0u : kMmRows * 16u);
-        constexpr int kGroups = S::kBHalves;              // W has one group of 128 rows
-        uint32_t it = 0, pair = 0;
+        constexpr int kGroups = kRt > S::kBHalves ? kRt : S::kBHalves;      // of 128 rows
+        const int groups = of_w ? kRt : S::kBHalves;
+        const uint8_t* scales = of_w ? a.w_scales : a.x_scales;
+        const int64_t rows = of_w ? a.n_out : a.tokens;
+        const uint32_t raw = base + S::kStages * S::kStage + (of_w ? 0u : kRt * 2048u);
+        // a lane copies what it will read itself: its own copies are all that it waits for
+        uint32_t ask_tile = blockIdx.x, ask_k = 0, ask_at = 0, at = 0;
+        int64_t ask_row = 0;
+        auto ask = [&] {
+            if (ask_tile < tiles) {
+                if (ask_k == 0) {
+                    uint32_t m, n;
+                    mm_tile(a, ask_tile, m, n);
+                    ask_row = (of_w ? (int64_t)m * S::kRows : (int64_t)n * kBn) + lane;
+                }
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    if (g >= groups) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t row = ask_row + 128 * g + 32 * i;
+                        const bool there = row < rows;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(raw + ask_at * S::kRaw + g * 2048u + (lane + 32 * i) * 16u),
+                                     "l"(there ? scales + row * a.pitch + ask_k * 8u : scales), "r"(there ? 16u : 0u) : "memory");
+                    }
+                }
+                ask_k += 2;
+                if (ask_k >= a.k_stages) { ask_k = 0; ask_tile += gridDim.x; }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            if (++ask_at == (uint32_t)kRawAhead) ask_at = 0;
+        };
+        for (int e = 0; e < kRawAhead - 1; ++e) ask();
+        uint32_t it = 0;
         for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
             ScaleQuad now[kGroups];
             for (uint32_t k = 0; k < a.k_stages && ok; ++k, ++it) {
                 if ((k & 1u) == 0u) {
-                    const uint32_t e = pair % S::kRawEntries;
-                    ok = __all_sync(0xffffffffu, mbar_wait_copies(raw_full + e, (pair / S::kRawEntries) & 1u));
-                    if (!ok) break;
+                    ask();
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kRawAhead - 1) : "memory");
 #pragma unroll
                     for (int g = 0; g < kGroups; ++g)
-                        if (g == 0 || !of_w) read_scales(now[g], from + e * S::kRaw + g * 2048u, lane);
-                    __syncwarp();
-                    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(raw_empty + e)) : "memory");
-                    ++pair;
+                        if (g < groups) read_scales(now[g], raw + at * S::kRaw + g * 2048u, lane);
+                    if (++at == (uint32_t)kRawAhead) at = 0;
                 }
                 const uint32_t s = it % S::kStages, round = it / S::kStages;
                 if (round > 0) ok = __all_sync(0xffffffffu, mbar_wait(empty + s, (round - 1u) & 1u));
                 if (!ok) break;
-                const uint32_t at = base + s * S::kStage + S::kA + S::kB + (of_w ? 0u : 2 * kScaleAtom);
+                const uint32_t at = base + s * S::kStage + S::kA + S::kB + (of_w ? 0u : 2 * kRt * kScaleAtom);
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
-                    if (g > 0 && of_w) continue;
+                    if (g >= groups) continue;
                     const uint32_t to = at + 2 * g * kScaleAtom, first = (k / 2) * 16u;
                     if ((k & 1u) == 0u) {
                         store_scales<0>(to, now[g], a.kb, first, lane);
@@ -206,9 +229,11 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(full + s)) : "memory");
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
+        // a quarter of the lanes each, of one accumulator, or of half of its columns where there is one
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        constexpr int kCols = kBn / 2;                    // of this warp
+        constexpr int kCols = kRt == 2 ? kBn : kBn / 2;   // of this warp
         uint32_t done = 0;
         for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++done) {
             uint32_t m, n;
@@ -222,12 +247,15 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             tc_fence_before();
             __syncwarp();
             if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(acc_empty)) : "memory");
-            const int64_t row = (int64_t)m * kMmRows + 32 * quarter + lane, token = (int64_t)n * kBn + half * kCols;
+            const int64_t row = (int64_t)m * S::kRows + (kRt == 2 ? 128 * half : 0) + 32 * quarter + lane, token = (int64_t)n * kBn + (kRt == 2 ? 0 : half * kCols);
             if (row < a.n_out) {
                 __nv_bfloat16* y = a.y + token * a.n_out + row;
+                const int left = (int)min((int64_t)kCols, a.tokens - token);
 #pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                    if (token + c < a.tokens) y[c * a.n_out] = __ushort_as_bfloat16((unsigned short)(v[c >> 1] >> (16 * (c & 1))));
+                for (int c = 0; c < kCols; ++c) {
+                    if (c < left) *y = __ushort_as_bfloat16((unsigned short)(v[c >> 1] >> (16 * (c & 1))));
+                    y += a.n_out;
+                }
             }
         }
     }
@@ -238,20 +266,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     if (warp == 1) tmem_dealloc(tmem, S::kTmem);
 }
 
-template <int kBn>
-int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes, const uint8_t* w_scales, int64_t k_in, MmArgs a,
-                   cudaStream_t st)
+template <int kRt, int kBn>
+int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* w_codes, int64_t k_in, MmArgs a, cudaStream_t st)
 {
-    CUtensorMap w_map, x_map, ws_map, xs_map;
-    const int64_t pitch = mx_code_pitch(k_in), scale_pitch = mx_scale_pitch(k_in);
-    if (!make_byte_map(ctx->device, w_scales, scale_pitch, a.n_out, 16, kMmRows, false, &ws_map) ||
-        !make_byte_map(ctx->device, x_scales, scale_pitch, a.tokens, 16, kBn, false, &xs_map)) return LLVQ_ECUDA;
-    if (!make_byte_map(ctx->device, w_codes, pitch, a.n_out, (int)kStageCodes, kMmRows, true, &w_map) ||
+    using S = MmShape<kRt, kBn>;
+    CUtensorMap w_map, x_map;
+    const int64_t pitch = mx_code_pitch(k_in);
+    if (!make_byte_map(ctx->device, w_codes, pitch, a.n_out, (int)kStageCodes, S::kRows, true, &w_map) ||
         !make_byte_map(ctx->device, x_codes, pitch, a.tokens, (int)kStageCodes, kBn, true, &x_map)) return LLVQ_ECUDA;
-    if (!set_smem<mx_gemm_kernel<kBn>>(ctx, MmShape<kBn>::kSmem)) return LLVQ_ECUDA;
+    if (!set_smem<mx_gemm_kernel<kRt, kBn>>(ctx, S::kSmem)) return LLVQ_ECUDA;
+    a.tiles_m = (uint32_t)((a.n_out + S::kRows - 1) / S::kRows);
     a.tiles_n = (uint32_t)((a.tokens + kBn - 1) / kBn);
     const unsigned grid = (unsigned)std::min<uint64_t>((uint64_t)a.tiles_m * a.tiles_n, (uint64_t)ctx->sm_count);
-    return launch_pdl(mx_gemm_kernel<kBn>, grid, kMmThreads, MmShape<kBn>::kSmem, st, w_map, x_map, ws_map, xs_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
+    return launch_pdl(mx_gemm_kernel<kRt, kBn>, grid, kMmThreads, S::kSmem, st, w_map, x_map, a) == cudaSuccess ? launch_status() : LLVQ_ECUDA;
 }
 
 }  // namespace
@@ -270,16 +297,21 @@ extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const
     cudaStream_t st = (cudaStream_t)stream;
     if (k_in == 0) return cudaMemsetAsync(d_y_bf16, 0, (size_t)n_out * tokens * 2, st) == cudaSuccess ? LLVQ_OK : LLVQ_ECUDA;
     MmArgs a{};
-    a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in);
-    a.k_stages = (a.kb + 7) / 8; a.tiles_m = (uint32_t)((n_out + kMmRows - 1) / kMmRows); a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
-    // The widest tile whose rounds over the SMs take least: a stage takes about 128 / 64 / 48 cycles per 64 columns with 256 / 128 / 64 tokens
-    // (the narrowest is held up by its reads of shared memory).
-    auto cost = [&](int bn, int cycles) {
-        const uint64_t t = (uint64_t)a.tiles_m * (uint64_t)((tokens + bn - 1) / bn);
-        return (t + ctx->sm_count - 1) / ctx->sm_count * cycles;
-    };
-    const uint64_t c256 = cost(256, 128), c128 = cost(128, 64), c64 = cost(64, 48);
-    if (c256 <= c128 && c256 <= c64) return launch_mx_gemm<256>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
-    if (c128 <= c64) return launch_mx_gemm<128>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
-    return launch_mx_gemm<64>(ctx, d_x_codes, d_x_scales, d_codes, d_scales, k_in, a, st);
+    a.w_scales = d_scales; a.x_scales = d_x_scales; a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in); a.pitch = (uint32_t)mx_scale_pitch(k_in);
+    a.k_stages = (a.kb + 7) / 8; a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
+    // The tile whose rounds over the SMs take least, at the cycles that a stage takes and some for the end of a tile, which writes it.
+    const struct { int rows, bn, stage, end; } shapes[4] = {{256, 224, 1600, 3000}, {128, 256, 1000, 1500}, {128, 128, 500, 1000}, {128, 64, 330, 700}};
+    int pick = 0;
+    uint64_t best = ~0ull;
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t tiles = (uint64_t)((n_out + shapes[i].rows - 1) / shapes[i].rows) * (uint64_t)((tokens + shapes[i].bn - 1) / shapes[i].bn);
+        const uint64_t cost = (tiles + ctx->sm_count - 1) / ctx->sm_count * ((uint64_t)a.k_stages * shapes[i].stage + shapes[i].end);
+        if (cost < best) { best = cost; pick = i; }
+    }
+    switch (pick) {
+        case 0: return launch_mx_gemm<2, 224>(ctx, d_x_codes, d_codes, k_in, a, st);
+        case 1: return launch_mx_gemm<1, 256>(ctx, d_x_codes, d_codes, k_in, a, st);
+        case 2: return launch_mx_gemm<1, 128>(ctx, d_x_codes, d_codes, k_in, a, st);
+        default: return launch_mx_gemm<1, 64>(ctx, d_x_codes, d_codes, k_in, a, st);
+    }
 }

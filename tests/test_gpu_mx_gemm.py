@@ -49,7 +49,7 @@ def test_product(P, ctx, tokens, n_out, k_in):
     check(y, x, w)
 
 
-@pytest.mark.parametrize("tokens,n_out,k_in", [(128, 19000, 288), (300, 18943, 256), (3000, 2000, 96), (2600, 4100, 544), (129, 20001, 1056)])
+@pytest.mark.parametrize("tokens,n_out,k_in", [(2017, 4300, 1300), (1000, 10000, 320), (448, 9472, 2080), (128, 19000, 288), (300, 18943, 256), (3000, 2000, 96), (2600, 4100, 544), (129, 20001, 1056)])
 def test_several_tiles_per_thread_block(P, ctx, tokens, n_out, k_in):
     y, x, w = run(P, ctx, tokens, n_out, k_in)
     check(y, x, w)
