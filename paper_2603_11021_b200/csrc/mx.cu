@@ -441,7 +441,7 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                 if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(empty + s)) : "memory");
                 next();
             }
-            if (!ok) break;
+            if (kg_n == 1 && !ok) break;
             const int64_t row0 = (int64_t)tile * rows;
             auto put = [&](int n, int64_t row, float v) {
                 if (n >= a.batch || row >= a.n_out) return;
@@ -459,7 +459,8 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                 for (int n = 0; n < kTiles; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) part[(kg * kTiles * 8 + n * 8 + 2 * t + (j & 1)) * (int)rows + rg * 16 + g + 8 * (j >> 1)] = acc[n][j];
-                asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+                ok = all_well(ok, kWarps * 32);
+                if (!ok) break;
                 for (int i = threadIdx.x; i < a.batch * (int)rows; i += kWarps * 32) {
                     const int n = i / (int)rows, r = i & (int)(rows - 1);
                     float v = 0.0f;

@@ -378,7 +378,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
             const uint64_t tile_begin = (uint64_t)tile * a.steps;
             it += a.steps - step;
             step = 0;
-            ok = __all_sync(0xffffffffu, mbar_wait_copies(&acc_full, done & 1u));
+            ok = all_well(mbar_wait_copies(&acc_full, done & 1u), 256);
             if (!ok) break;
             tc_fence_after();
             const uint32_t from = share_owner(units, gridDim.x, tile_begin), to = share_owner(units, gridDim.x, tile_begin + a.steps - 1);

@@ -20,6 +20,15 @@ __device__ __forceinline__ bool elect_one()
 // The warp's number, known to the compiler to be the same for all its lanes.
 __device__ __forceinline__ int warp_number() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
 
+// Named barrier 1 for `threads` threads, which also learn whether all of them are well: where one's wait ran out, all leave together, so that nobody is left
+// at a barrier.
+__device__ __forceinline__ bool all_well(bool well, int threads)
+{
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.and.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((uint32_t)well), "r"(threads) : "memory");
+    return r != 0u;
+}
+
 // 512 bytes of scales from shared memory to four columns of tensor memory, for all four quarters of its lanes.
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint64_t desc)      // desc = smem_desc(address, 0, 128)
 {

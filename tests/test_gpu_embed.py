@@ -225,3 +225,28 @@ def test_lookup_then_head_then_gradient(P, ctx):
     grad = P.llvq_embed_grad(ctx, x, tokens, vocab, scale=dim ** 0.5)
     check_grad(grad, x, tokens, vocab, dim ** 0.5)
     assert P.llvq_last_error(ctx) == (0, 0)
+
+
+def test_rows_behind_2_to_the_31_elements(P, ctx):
+    vocab, dim = 280000, 8192                              # 4.6 GB in bf16, 9.2 GB of gradient
+    table = torch.zeros((vocab, dim), dtype=torch.bfloat16, device="cuda")
+    far = torch.tensor([vocab - 1, 5, vocab - 1, 270001], device="cuda")
+    table[far] = torch.randn((4, dim), device="cuda").bfloat16()
+    assert torch.equal(P.llvq_embed(ctx, table, far), table[far])
+    dy = torch.randn((4, dim), device="cuda")
+    grad = P.llvq_embed_grad(ctx, dy, far, vocab)
+    assert torch.equal(grad[5], dy[1]) and torch.equal(grad[270001], dy[3])
+    assert ((grad[vocab - 1] - (dy[0] + dy[2])).abs() <= 2.0 ** -23 * (dy[0].abs() + dy[2].abs())).all()
+    assert (grad[[0, 4, 6, 270000, 270002, vocab - 2]] == 0).all()
+    del grad, table
+    codes, scales = P.llvq_mx_quantize(ctx, torch.ones((1, dim), device="cuda"))
+    codes = codes.expand(600000, -1).contiguous()          # 2.5 GB of codes
+    scales = scales.expand(600000, -1).contiguous()
+    scales[599999] += 1
+    x = torch.ones(dim, device="cuda").bfloat16()
+    y = P.llvq_mx_gemv(ctx, codes, scales, 600000, dim, x)
+    assert (y[:-1] == dim).all() and y[-1] == 2 * dim
+    y = P.llvq_mx_gemm_small_batch(ctx, codes, scales, 600000, dim, x.expand(40, -1).contiguous())
+    assert (y[:, :-1] == dim).all() and (y[:, -1] == 2 * dim).all()
+    out = P.llvq_mx_embed(ctx, codes, scales, 600000, dim, torch.tensor([599999, 0], device="cuda"))
+    assert (out[0] == 2).all() and (out[1] == 1).all()
