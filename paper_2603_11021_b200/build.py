@@ -80,7 +80,7 @@ def _build_native() -> None:
         f'-DLLVQ_BUILT_FOR="{native_stamp()}"',
         "-I", os.path.join(ROOT, "include"), "-I", os.path.join(root, "include"), "-I", os.path.join(root, "include", "torch", "csrc", "api", "include"),
         "-I", os.path.join(cuda, "include"), "-I", sysconfig.get_paths()["include"], BINDING, "-o", tmp, "-L", PKG, "-lllvq",
-        "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"])
+        "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN"])
     os.replace(tmp, NATIVE)
 
 
