@@ -299,8 +299,9 @@ extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const
     MmArgs a{};
     a.w_scales = d_scales; a.x_scales = d_x_scales; a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in); a.pitch = (uint32_t)mx_scale_pitch(k_in);
     a.k_stages = (a.kb + 7) / 8; a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
-    // The tile whose rounds over the SMs take least, at the cycles that a stage takes and some for the end of a tile, which writes it.
-    const struct { int rows, bn, stage, end; } shapes[4] = {{256, 224, 1600, 3000}, {128, 256, 1000, 1500}, {128, 128, 500, 1000}, {128, 64, 330, 700}};
+    // The tile whose rounds over the SMs take least, at the cycles that a stage takes and some for the end of a tile, which writes it.  us with the four:
+    // 28672 x 8192 x 2048 tokens 221, 226, 257, 423; 8192 x 8192 x 4096 142, 135, 156, 259; 4096 x 11008 x 512 36, 26, 20, 30; 4096 x 4096 x 237 18, 12, 9.0, 8.8.
+    const struct { int rows, bn, stage, end; } shapes[4] = {{256, 224, 1450, 4500}, {128, 256, 970, 1500}, {128, 128, 560, 1000}, {128, 64, 420, 700}};
     int pick = 0;
     uint64_t best = ~0ull;
     for (int i = 0; i < 4; ++i) {

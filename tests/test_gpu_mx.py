@@ -131,7 +131,7 @@ def test_an_infinity_in_the_activations(P, ctx, batch):
     clean = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 300, 480, x.cuda())
     x[0, 77] = float("inf")
     y = f64(P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 300, 480, x.cuda()))
-    want = np.where(w[:, 77] == 0, np.nan, np.sign(w[:, 77]) * np.inf)
+    want = np.where(w[:, 77] == 0, np.nan, np.where(w[:, 77] < 0, -np.inf, np.inf))
     assert np.array_equal(y[0], want, equal_nan=True) and np.array_equal(y[1:], f64(clean)[1:])
 
 
@@ -144,6 +144,19 @@ def test_activations_of_very_different_sizes(P, ctx, batch):
     x[:, 100] = 2.0 ** 17
     x[:, 101] = 0
     x = torch.where(x.abs() < 2.0 ** -2, torch.zeros_like(x), x)
+    y = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 64, 480, x.cuda())
+    check_product(y, f64(x), mx.values_of(codes, scales, 480))
+
+
+@pytest.mark.parametrize("batch", [1, 3, 16])
+def test_activations_that_become_subnormal_binary16(P, ctx, batch):
+    # one channel 2^28 to 2^30 times the others, where every weight is zero: up to 16 rows of X are exact down to 2^-32 of the largest
+    codes, scales = mx.random_matrix(64, 480, seed=3)
+    codes[:, 50] = 0                                          # columns 100 and 101
+    x = torch.randn((batch, 480), generator=torch.Generator().manual_seed(1)).bfloat16()
+    x = torch.where(x.abs() < 2.0 ** -2, torch.zeros_like(x), x)
+    x[:, 100] = 2.0 ** 28
+    x[:, 101] = 0
     y = P.llvq_mx_gemm_small_batch(ctx, dev(codes), dev(scales), 64, 480, x.cuda())
     check_product(y, f64(x), mx.values_of(codes, scales, 480))
 
