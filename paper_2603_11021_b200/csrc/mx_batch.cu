@@ -25,7 +25,8 @@ using namespace llvq;
 //               instruction takes 4-bit operands
 //   warp 16     the scales of W    warp 18: X    warp 19: the MMAs, eight per step    warps 0-7: the accumulators and Y
 // It begins to read W while the first kernel still runs (which waits for everything before it first).
-// Bound by HBM for few rows of X; at 64 the products, and reading X out of L2 for every tile, take as long.
+// Bound by shared memory at 64 rows of X (28672 x 8192: 54.6 us, 0.75 us or 1400 cycles a step): per step the MMAs read 80 KB (640 cycles at 128 bytes), codes
+// are written, read and spread (512, the spread ones into every other pair of banks), X is written (200).  Fewer rows of X: by that and the latency of HBM.
 constexpr int kBatchRows = 256, kBatchCols = 128, kBatchThreads = 640;
 constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a step's weights as operand, a byte of room per element
 constexpr uint32_t kBatchCode = kBatchA / 2;              // and as they are stored
