@@ -244,8 +244,6 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(codes + in.at * kBatchCode + p * 16u + i * 2048u) : "memory");
-            __syncwarp();
-            if (lane == 0) arrive(code_empty + in.at);
             if (it >= stages) ok = __all_sync(0xffffffffu, mbar_wait(empty + out.at, out.phase ^ 1u));
             if (!ok) break;
             const uint32_t at = base + out.at * kStage + to;
@@ -256,7 +254,9 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
             }
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) arrive(full + out.at);
+            // The codes' place is given back only now: the stores above had what was read in their registers.  Right behind the loads, other lanes' loads may
+            // still be on their way, and where shared memory is busy the next codes overtake them.
+            if (lane == 0) { arrive(full + out.at); arrive(code_empty + in.at); }
             in.next(kBatchPacked, 2u);
             out.next(stages, 2u);
         }
@@ -298,10 +298,9 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
                 if (!ok) break;
                 read_scales(now[0], raw + box.at * (kBatchRows * 16u), lane);
                 read_scales(now[1], raw + box.at * (kBatchRows * 16u) + 2048u, lane);
-                __syncwarp();
                 box.next(kRawScales);
-                ask();
             }
+            const bool was_fresh = fresh;
             fresh = (step & 3u) == 3u || step + 1u == a.steps;
             if (it >= stages) ok = __all_sync(0xffffffffu, mbar_wait(empty + out.at, out.phase ^ 1u));
             if (!ok) break;
@@ -319,6 +318,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
             fence_async_smem();
             __syncwarp();
             if (lane == 0) arrive(full + out.at);
+            if (was_fresh) ask();                         // into the box's place: the stores above had a part of every load in their registers
             out.next(stages);
             advance();
         }

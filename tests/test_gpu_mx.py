@@ -215,6 +215,20 @@ def test_products_are_the_same_every_time_and_touch_nothing_else(P, ctx):
             assert torch.equal(P.llvq_mx_gemm_small_batch(ctx, codes, scales, 1000, 4096, x).view(-1), y[4:-4])
 
 
+@pytest.mark.parametrize("n_out,k_in,batch", [(10311, 8290, 20), (10311, 8290, 48), (20000, 4096, 64), (4096, 11004, 5), (11008, 4096, 1)])
+def test_products_are_the_same_many_times(P, ctx, n_out, k_in, batch):
+    # busy shared memory: a place that is given back before all lanes have read it showed in about one call of a hundred
+    g = torch.Generator(device="cuda").manual_seed(5)
+    codes = torch.randint(0, 256, (n_out, mx.blocks(k_in) * 16), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.randint(110, 125, (n_out, mx.pitch(k_in)), dtype=torch.uint8, device="cuda", generator=g)
+    x = torch.randn((batch, k_in), device="cuda", generator=g).bfloat16()
+    first = P.llvq_mx_gemm_small_batch(ctx, codes, scales, n_out, k_in, x)
+    same = torch.ones((), dtype=torch.bool, device="cuda")
+    for _ in range(400):
+        same &= (P.llvq_mx_gemm_small_batch(ctx, codes, scales, n_out, k_in, x) == first).all()
+    assert bool(same)
+
+
 def test_nothing_to_do(P, ctx):
     none = torch.empty((0, 0), dtype=torch.uint8, device="cuda")
     c, s = P.llvq_mx_quantize(ctx, torch.empty((0, 64), device="cuda"))
