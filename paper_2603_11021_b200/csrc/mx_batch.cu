@@ -348,7 +348,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
                 ok = __all_sync(0xffffffffu, mbar_wait_copies(x_full + x.at, x.phase) && mbar_wait_copies(full + in.at, in.phase));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + (it & 1u) * 16u, tb = ta + 8u;
+                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + in.at * 16u, tb = ta + 8u;      // scales have a place per stage, like the operands
                 const uint64_t da = da0 + off, db = db0 + x_off, sa = sa0 + off, sb = sb0 + x_off;
                 if (elect_one()) {
                     scales_to_tmem(ta, sa);

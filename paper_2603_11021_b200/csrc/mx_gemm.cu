@@ -17,7 +17,7 @@ using namespace llvq;
 //   warp 1      copies the scales to tensor memory and issues four MMAs of 64 columns per 128 rows and stage
 //   warps 4-11  take the accumulators out as bf16, hand them back, then write Y
 // Large products are bound by what TMA and L2 bring, so the large tile is the one that reads least per product: 256 rows by 224 tokens fill tensor
-// memory with two accumulators and two stages' scales (60 KB per stage for 1.75 times the products of 128 x 256, which reads 48 KB).  There is one set
+// memory with two accumulators and the scales of two stages (60 KB per stage for 1.75 times the products of 128 x 256, which reads 48 KB).  There is one set
 // of accumulators: taking it out costs the tensor cores a few hundred of the tens of thousands of cycles of a tile.
 constexpr int kMmThreads = 384;
 constexpr int kMmGroup = 16;                              // row tiles that are walked together, for L2
@@ -31,7 +31,8 @@ template <int kRt, int kBn> struct MmShape {
     static constexpr uint32_t kStage = kA + kB + kScales; // a multiple of 1024
     static constexpr int kStages = kRt == 2 ? 3 : kBn == 256 ? 4 : kBn == 128 ? 6 : 7;
     static constexpr uint32_t kScaleCols = 8 * (kRt + kBHalves);               // columns of tensor memory that a stage's scales take
-    static constexpr uint32_t kCols = kRt * kBn + 2 * kScaleCols, kTmem = kCols > 256 ? 512 : kCols > 128 ? 256 : 128;
+    static constexpr int kScaleBufs = kRt == 2 ? 2 : kStages;                  // a place per stage where tensor memory has them
+    static constexpr uint32_t kCols = kRt * kBn + kScaleBufs * kScaleCols, kTmem = kCols > 256 ? 512 : kCols > 128 ? 256 : 128;
     static constexpr uint32_t kRaw = (kRt + kBHalves) * 128 * 16;      // scales as they come, of two stages
     static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage + kRawAhead * kRaw + 256;
     static_assert(kStage % 1024 == 0 && kCols <= kTmem && kSmem <= 227 * 1024, "");
@@ -128,13 +129,19 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             }
         }
     } else if (warp == 1) {
-        uint32_t done = 0, s = 0, phase = 0, buffer = 0;
+        uint32_t done = 0, s = 0, phase = 0, buffer = 0, it = 0, old = 0, old_phase = 0;
         const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + S::kA), sc0 = smem_desc(base + S::kA + S::kB, 0u, 128u);
         for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++done) {
             if (done > 0) ok = __all_sync(0xffffffffu, mbar_wait(acc_empty, (done - 1u) & 1u));
             for (uint32_t k = 0; k < a.k_stages && ok; ++k) {
                 ok = __all_sync(0xffffffffu, mbar_wait_copies(full + s, phase));
                 if (!ok) break;
+                // fewer places of scales than stages: the MMAs that read this one are waited for (those of the stage before are still running)
+                if (S::kScaleBufs < S::kStages && it >= (uint32_t)S::kScaleBufs) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(empty + old, old_phase));
+                    if (!ok) break;
+                    if (++old == (uint32_t)S::kStages) { old = 0; old_phase ^= 1u; }
+                }
                 tc_fence_after();
                 const uint32_t off = s * (S::kStage >> 4), ta = tmem + kRt * kBn + buffer * S::kScaleCols, tb = ta + 8 * kRt;
                 const uint64_t da = da0 + off, db = db0 + off, sc = sc0 + off;
@@ -155,7 +162,8 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                     umma_commit(empty + s);
                 }
                 __syncwarp();
-                buffer ^= 1u;
+                ++it;
+                if (++buffer == (uint32_t)S::kScaleBufs) buffer = 0;
                 if (++s == (uint32_t)S::kStages) { s = 0; phase ^= 1u; }
             }
             if (ok && elect_one()) umma_commit(acc_full);
