@@ -25,7 +25,7 @@ using namespace llvq;
 //               instruction takes 4-bit operands
 //   warp 16     the scales of W    warp 18: X    warp 19: the MMAs, eight per step    warps 0-7: the accumulators and Y
 // It begins to read W while the first kernel still runs (which waits for everything before it first).
-// Bound by shared memory at 64 rows of X (28672 x 8192: 54.6 us, 0.75 us or 1400 cycles a step): per step the MMAs read 80 KB (640 cycles at 128 bytes), codes
+// Bound by shared memory at 64 rows of X (28672 x 8192: 54.9 us, 0.75 us or 1400 cycles a step): per step the MMAs read 80 KB (640 cycles at 128 bytes), codes
 // are written, read and spread (512, the spread ones into every other pair of banks), X is written (200).  Fewer rows of X: by that and the latency of HBM.
 constexpr int kBatchRows = 256, kBatchCols = 128, kBatchThreads = 640;
 constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a step's weights as operand, a byte of room per element
@@ -348,7 +348,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
                 ok = __all_sync(0xffffffffu, mbar_wait_copies(x_full + x.at, x.phase) && mbar_wait_copies(full + in.at, in.phase));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + in.at * 16u, tb = ta + 8u;      // scales have a place per stage, like the operands
+                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + (stages == 2u ? it & 1u : in.at) * 16u, tb = ta + 8u;      // a place of scales per stage
                 const uint64_t da = da0 + off, db = db0 + x_off, sa = sa0 + off, sb = sb0 + x_off;
                 if (elect_one()) {
                     scales_to_tmem(ta, sa);

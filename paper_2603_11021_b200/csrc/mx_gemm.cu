@@ -129,7 +129,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             }
         }
     } else if (warp == 1) {
-        uint32_t done = 0, s = 0, phase = 0, buffer = 0, it = 0, old = 0, old_phase = 0;
+        uint32_t done = 0, s = 0, phase = 0, it = 0, old = 0, old_phase = 0;
         const uint64_t da0 = smem_desc_sw128(base), db0 = smem_desc_sw128(base + S::kA), sc0 = smem_desc(base + S::kA + S::kB, 0u, 128u);
         for (uint32_t tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x, ++done) {
             if (done > 0) ok = __all_sync(0xffffffffu, mbar_wait(acc_empty, (done - 1u) & 1u));
@@ -143,7 +143,7 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                     if (++old == (uint32_t)S::kStages) { old = 0; old_phase ^= 1u; }
                 }
                 tc_fence_after();
-                const uint32_t off = s * (S::kStage >> 4), ta = tmem + kRt * kBn + buffer * S::kScaleCols, tb = ta + 8 * kRt;
+                const uint32_t off = s * (S::kStage >> 4), ta = tmem + kRt * kBn + (S::kScaleBufs == 2 ? it & 1u : s) * S::kScaleCols, tb = ta + 8 * kRt;
                 const uint64_t da = da0 + off, db = db0 + off, sc = sc0 + off;
                 if (elect_one()) {
 #pragma unroll
@@ -163,7 +163,6 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 }
                 __syncwarp();
                 ++it;
-                if (++buffer == (uint32_t)S::kScaleBufs) buffer = 0;
                 if (++s == (uint32_t)S::kStages) { s = 0; phase ^= 1u; }
             }
             if (ok && elect_one()) umma_commit(acc_full);
