@@ -167,28 +167,50 @@ __device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.a
 __device__ __forceinline__ uint64_t share_begin(uint64_t units, uint32_t blocks, uint32_t i) { return units * i / blocks; }
 __device__ __forceinline__ uint32_t share_owner(uint64_t units, uint32_t blocks, uint64_t u) { return (uint32_t)(((u + 1) * blocks - 1) / units); }
 
-// One result in binary32, product by product: for rows of X with an infinity, which the three terms cannot hold.
-__device__ __noinline__ float dot_plain(const BatchArgs& a, int64_t row, int n)
-{
-    float sum = 0.0f;
-    for (int64_t k = 0; k < a.k_in; ++k) {
-        const uint32_t byte = a.codes[row * a.code_pitch + (k >> 1)], e = a.scales[row * a.scale_pitch + (k >> 5)];
-        float v[8];
-        mx_expand8((byte >> (4 * (k & 1))) & 15u, v);
-        sum += v[0] * mx_scale_value(e) * __bfloat162float(a.x[(int64_t)n * a.k_in + k]);
-    }
-    return sum;
-}
-
 __device__ __forceinline__ void put_y(const BatchArgs& a, int64_t row, int n, float v) { a.y[(int64_t)n * a.n_out + row] = __float2bfloat16_rn(v); }
 
-// Where a result is NaN: rows of X with an infinity (and no NaN) once more.
-__device__ __noinline__ void mend_row(const BatchArgs& a, int64_t row)
+// Eight bits to the highest bits of eight nibbles.
+__device__ __forceinline__ uint32_t nibble_tops(uint32_t bits)
 {
-    for (int n = 0; n < a.batch; ++n) {
-        bool nan = false, inf = false;
-        for (uint32_t c = 0; c < a.steps; ++c) { const uint8_t note = a.notes[(uint64_t)c * a.batch + n]; nan |= note == 2; inf |= note == 1; }
-        if (inf && !nan) put_y(a, row, n, dot_plain(a, row, n));
+    bits = (bits | bits << 12) & 0x000f000fu;
+    bits = (bits | bits << 6) & 0x03030303u;
+    return ((bits | bits << 3) & 0x11111111u) << 3;
+}
+
+// Rows of X that hold an infinity and no NaN (bits of `rows`), which the three terms cannot hold, for one row of W per thread: infinity times what is not
+// zero is an infinity, times zero NaN, and what is finite does not matter beside it.  So signs and zeros of the codes that meet an infinity decide, 32 of
+// them at a time: one load of a row's block per thread, and the infinities of a block of X by ballot.  All lanes of the warp come here.
+__device__ __noinline__ void mend_row(const BatchArgs& a, uint64_t rows, int64_t row)
+{
+    const int lane = threadIdx.x & 31;
+    const bool there = row < a.n_out;
+    const uint8_t* codes = a.codes + (there ? row : 0) * a.code_pitch;
+    const uint8_t* scales = a.scales + (there ? row : 0) * a.scale_pitch;
+    bool nan = !there;                                    // a block that is NaN, wherever it is
+    for (uint32_t b = 0; b < a.kb; ++b) nan |= scales[b] == 255;
+    for (; rows; rows &= rows - 1u) {
+        const int n = __ffsll((long long)rows) - 1;
+        const unsigned short* x = reinterpret_cast<const unsigned short*>(a.x) + (int64_t)n * a.k_in;
+        bool up = nan, down = nan;                        // products that are +inf and -inf; both: NaN
+        for (uint32_t c = 0; c < a.steps && !__all_sync(0xffffffffu, up && down); ++c) {
+            if (a.notes[(uint64_t)c * a.batch + n] != 1u) continue;
+            for (uint32_t b = 4u * c; b < min(4u * c + 4u, a.kb); ++b) {
+                const int64_t k = (int64_t)b * kMxBlock + lane;
+                const uint32_t v = k < a.k_in ? x[k] : 0u;
+                const uint32_t plus = __ballot_sync(0xffffffffu, v == 0x7f80u), minus = __ballot_sync(0xffffffffu, v == 0xff80u);
+                if ((plus | minus) == 0u) continue;
+                const uint4 block = *reinterpret_cast<const uint4*>(codes + (int64_t)b * kMxBlockBytes);
+                const uint32_t w[4] = {block.x, block.y, block.z, block.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t p = nibble_tops(plus >> (8 * i) & 255u), m = nibble_tops(minus >> (8 * i) & 255u), some = (w[i] & 0x77777777u) + 0x77777777u;
+                    const bool zero = ((p | m) & ~some) != 0u;
+                    up |= zero || ((p & ~w[i]) | (m & w[i])) != 0u;
+                    down |= zero || ((p & w[i]) | (m & ~w[i])) != 0u;
+                }
+            }
+        }
+        if (there) put_y(a, row, n, __uint_as_float(up && down ? 0x7fc00000u : up ? 0x7f800000u : 0xff800000u));
     }
 }
 
@@ -205,6 +227,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
     extern __shared__ uint8_t mb_smem[];
     __shared__ uint64_t code_full[kBatchPacked], code_empty[kBatchPacked], full[3], empty[3], x_full[kBatchX], x_empty[kBatchX], raw_full[kRawScales], acc_full, acc_empty;
     __shared__ uint32_t tmem_slot, last_slot;
+    __shared__ unsigned long long mend_rows;
     const uint32_t base = (smem_u32(mb_smem) + 1023u) & ~1023u, stages = a.stages;
     const uint32_t x_bytes = batch_x_bytes(a.npad), codes = base + stages * kStage, raw = codes + kBatchPacked * kBatchCode, x_at = raw + kRawScales * kBatchRows * 16u;
     const int warp = warp_number(), lane = threadIdx.x & 31;
@@ -374,7 +397,7 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
         }
     } else {
         pdl_wait();
-        uint32_t done = 0;
+        uint32_t done = 0, odd_from = 0xffffffffu, odd_to = 0;      // the first and last tile with a result of this block's that is NaN
         for (; it < total; ++tile, ++done) {
             const uint64_t tile_begin = (uint64_t)tile * a.steps;
             it += a.steps - step;
@@ -440,7 +463,24 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
                 }
                 asm volatile("bar.sync 1, 256;" ::: "memory");
             }
-            if (odd) mend_row(a, row);
+            if (odd) { odd_from = min(odd_from, tile); odd_to = tile; }
+        }
+        // Behind all tiles, where nobody waits for these warps: in between, rows full of infinities let the waits of the others run out.  A row of X with an
+        // infinity is NaN in every result so far, so the first and last tile where one was seen are tiles that this block has written, as are all between them.
+        if (ok && !all_well(odd_from == 0xffffffffu, 256)) {
+            if (threadIdx.x == 0) mend_rows = 0ull;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            for (int n = warp; n < a.batch; n += 8) {
+                uint32_t notes = 0;
+                for (uint32_t c = lane; c < a.steps; c += 32) notes |= a.notes[(uint64_t)c * a.batch + n];
+                if (__reduce_or_sync(0xffffffffu, notes) == 1u && lane == 0) atomicOr(&mend_rows, 1ull << n);
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const uint64_t rows = mend_rows;
+            odd_from = __reduce_min_sync(0xffffffffu, odd_from);
+            odd_to = __reduce_max_sync(0xffffffffu, odd_to);
+            if (rows != 0u && odd_from != 0xffffffffu)
+                for (uint32_t t = odd_from; t <= odd_to; ++t) mend_row(a, rows, (int64_t)t * kBatchRows + warp * 32 + lane);
         }
     }
     if (!ok) atomicOr(a.flags, (uint32_t)LLVQ_FLAG_WAIT_TIMEOUT);
