@@ -215,14 +215,15 @@ __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor)
     return f16_pair(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
 }
 
-// The 512 columns of a chunk of a row of X as they were loaded (columns 8 lane .. and 256 + 8 lane ..) to binary16, in place; the exponent of the factor.
+// The 512 columns of a chunk of a row of X as they were loaded (columns 8 lane .. and 256 + 8 lane ..) to binary16, in place; the exponent of the factor,
+// at most 125 (which leaves every number below 2^-111 exact), and 0 where no finite number but zero is among them.
 __device__ __forceinline__ int chunk_to_f16(uint4 v[2])
 {
     uint32_t m = 0;
 #pragma unroll
     for (int h = 0; h < 2; ++h) m = max_finite(max_finite(max_finite(max_finite(m, v[h].x), v[h].y), v[h].z), v[h].w);
     m = __reduce_max_sync(0xffffffffu, m);
-    const int f = min(14 - ((int)(m >> 7) - 127), 127);
+    const int f = m == 0u ? 0 : min(14 - ((int)(m >> 7) - 127), 125);
     const float factor = __uint_as_float((uint32_t)(f + 127) << 23);
 #pragma unroll
     for (int h = 0; h < 2; ++h) v[h] = make_uint4(to_f16(v[h].x, factor), to_f16(v[h].y, factor), to_f16(v[h].z, factor), to_f16(v[h].w, factor));
@@ -251,7 +252,7 @@ mx_stream_split_kernel(MxStream a)
 // d * 2^h in two steps, for h that binary32 may not hold; NaN for the scale byte 255
 __device__ __forceinline__ float scale_far(float d, uint32_t e, int f)
 {
-    const int h = (int)e - 127 - f, h1 = h / 2, h2 = h - h1;               // |h| <= 127 + 128 + 127 + ...: both halves are normal exponents
+    const int h = (int)e - 127 - f, h1 = h / 2, h2 = h - h1;               // -127 - 125 <= h <= 127 + 113: both halves are normal exponents
     const float s1 = e == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(h1 + 127) << 23);
     return d * s1 * __uint_as_float((uint32_t)(h2 + 127) << 23);
 }

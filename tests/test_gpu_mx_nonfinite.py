@@ -93,3 +93,22 @@ def test_infinities_and_nan_here_and_there(P, ctx, n_out, k_in, batch):
     y = P.llvq_mx_gemm_small_batch(ctx, torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), n_out, k_in, x)
     check(y, x, w)
     assert P.llvq_last_error(ctx) == (0, 0)
+
+@pytest.mark.parametrize("batch", [1, 3, 8, 16])
+@pytest.mark.parametrize("others", [0.0, 2.0 ** -133, 2.0 ** -126])
+@pytest.mark.parametrize("scale", [0, 1, 2, 254])
+def test_an_infinity_among_zeros_meets_the_smallest_scales(P, ctx, batch, others, scale):
+    # columns 0 to 511 of X hold nothing else, or the smallest numbers there are: the smallest scale is 2^-127, and times an infinity it is one
+    n_out, k_in = 40, 520
+    codes, scales = mx.random_matrix(n_out, k_in, seed=3)
+    codes[:20] |= 0x11
+    codes[:, k_in // 2:] = 0
+    scales[:, :16] = scale
+    w = torch.from_numpy(mx.values_of(codes, scales, k_in)).float().cuda()
+    x = torch.full((batch, k_in), others)
+    x[0, 77] = INF
+    x[batch - 1, 200] = -INF
+    x = x.bfloat16().cuda()
+    codes, scales = torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda()
+    check(P.llvq_mx_gemm_small_batch(ctx, codes, scales, n_out, k_in, x), x, w)
+    check(P.llvq_mx_gemv(ctx, codes, scales, n_out, k_in, x[0])[None], x[:1], w)
