@@ -111,8 +111,9 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, uint32_t cols, int64_t
 // Y[n][r] = sum_k X[n][k] W[r][k] on m16n8k16 tiles in binary16: 16 rows of W against 8 of X.  An e2m1 element is a binary16 number that one
 // instruction per two elements makes; the scale of a block of 32 multiplies the block's sum in binary32.  Activations become binary16 as well:
 // the 512 columns of a chunk of a row of X are multiplied with the power of two that brings their largest finite magnitude to [2^14, 2^15), which
-// leaves every bf16 number exact down to 2^-32 of that magnitude and puts smaller ones off by at most 2^-40 of it, far below the rounding of
-// the sums (binary32, 2^-24 of the same magnitude).
+// leaves every bf16 number exact down to 2^-31 of that magnitude and puts smaller ones off by at most 2^-39 of it, far below the rounding of
+// the sums (binary32, 2^-24 of the same magnitude).  Where a weight of zero takes the largest out of the sum, those of other blocks are what counts: if a number
+// that would not be exact is in a block of 32 whose largest is below 2^-12 of the chunk's, every block of the chunk has a factor of its own.
 //
 // A thread block streams W: kWarps warps multiply, 16 rows by 512 columns each per stage, RG x 16 rows by KG x 512 columns together, RG x KG = kWarps.
 // The next warp copies their codes with TMA (rows of 128 bytes, swizzled, so that ldmatrix reads 16 bytes of eight rows without conflicts and hands each
@@ -122,7 +123,9 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, uint32_t cols, int64_t
 // one row, 54 us, 79 % of the measured bandwidth); beyond, the products do.
 constexpr int kChunk = 512;                              // columns of a warp's part of a stage
 constexpr int kXWarps = 4;
-constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice; the exponent is behind the columns
+constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice; the exponent is behind the columns,
+constexpr uint32_t kXOwn = kChunk * 2 + 16;              // and here, where it is kOwn, those of the 16 blocks, a byte each
+constexpr int kOwn = 1000;
 template <int kWarps, bool kPre> struct Stream {         // kWarps multiply; kPre: X comes as mx_stream_split_kernel left it
     static constexpr int kThreads = (kWarps + 1 + (kPre ? 1 : kXWarps)) * 32;
     static constexpr uint32_t kCodes = kWarps * 16 * (kChunk / 2), kScales = kWarps * 16 * 16;      // bytes per stage, whatever RG and KG
@@ -157,6 +160,13 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr)
 {
     uint32_t v;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ int lds_s8(uint32_t addr)
+{
+    int v;
+    asm volatile("ld.shared.s8 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
 
@@ -203,30 +213,64 @@ __device__ __forceinline__ uint4 load_x8(const MxStream& a, int n, int64_t k)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The larger of m and the magnitudes of two bf16, infinities and NaN left out (as bf16 bits).
-__device__ __forceinline__ uint32_t max_finite(uint32_t m, uint32_t pair)
+// Largest and smallest magnitudes of pairs of bf16, per half of a word.  most: 0x80 more than the largest finite one (an infinity or a NaN becomes negative);
+// least: one less than the smallest that is not zero (zero becomes the largest of all).
+constexpr uint32_t kMostNone = 0x00800080u, kLeastNone = 0xffffffffu;
+__device__ __forceinline__ void most_and_least(uint32_t& most, uint32_t& least, const uint4& v)
 {
-    const uint32_t lo = pair & 0x7fffu, hi = (pair >> 16) & 0x7fffu;
-    return max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t size = w[i] & 0x7fff7fffu;
+        most = __viaddmax_s16x2(size, 0x00800080u, most);
+        least = __viaddmin_u16x2(size, 0xffffffffu, least);
+    }
 }
+__device__ __forceinline__ uint32_t most_of(uint32_t most) { return max(most & 0xffffu, most >> 16) - 0x80u; }
+__device__ __forceinline__ uint32_t least_of(uint32_t least) { return min(least & 0xffffu, least >> 16) + 1u; }
 
 __device__ __forceinline__ uint32_t to_f16(uint32_t pair, float factor)
 {
     return f16_pair(__uint_as_float(pair << 16) * factor, __uint_as_float(pair & 0xffff0000u) * factor);
 }
 
-// The 512 columns of a chunk of a row of X as they were loaded (columns 8 lane .. and 256 + 8 lane ..) to binary16, in place; the exponent of the factor,
-// at most 125 (which leaves every number below 2^-111 exact), and 0 where no finite number but zero is among them.
-__device__ __forceinline__ int chunk_to_f16(uint4 v[2])
+// The exponent of the factor for a largest finite magnitude m (as bf16 bits): at most 125 (which leaves all numbers below 2^-110 exact), and 0 where m is zero.
+__device__ __forceinline__ int factor_of(uint32_t m) { return m == 0u ? 0 : min(14 - ((int)(m >> 7) - 127), 125); }
+
+__device__ __forceinline__ void half_to_f16(uint4& v, int f)
 {
-    uint32_t m = 0;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) m = max_finite(max_finite(max_finite(max_finite(m, v[h].x), v[h].y), v[h].z), v[h].w);
-    m = __reduce_max_sync(0xffffffffu, m);
-    const int f = m == 0u ? 0 : min(14 - ((int)(m >> 7) - 127), 125);
     const float factor = __uint_as_float((uint32_t)(f + 127) << 23);
+    v = make_uint4(to_f16(v.x, factor), to_f16(v.y, factor), to_f16(v.z, factor), to_f16(v.w, factor));
+}
+
+// The 512 columns of a chunk of a row of X as they were loaded (columns 8 lane .. and 256 + 8 lane ..) to binary16, in place; the exponent of the factor,
+// or kOwn where blocks have their own: then own[h] is that of the block of v[h].
+__device__ __forceinline__ int chunk_to_f16(uint4 v[2], int own[2])
+{
+    uint32_t most[2] = {kMostNone, kMostNone}, least[2] = {kLeastNone, kLeastNone};
+    most_and_least(most[0], least[0], v[0]);
+    most_and_least(most[1], least[1], v[1]);
+    const uint32_t m = __reduce_max_sync(0xffffffffu, most_of(__vmaxu2(most[0], most[1]))), exponent = m >> 7;
+    auto inexact = [&](uint32_t smallest) { return exponent > max(smallest >> 7, 1u) + 31u; };      // its last bit is below 2^-24, binary16's smallest step
+    if (__any_sync(0xffffffffu, inexact(least_of(__vminu2(least[0], least[1]))))) {      // seldom so
+        bool differ = false;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) v[h] = make_uint4(to_f16(v[h].x, factor), to_f16(v[h].y, factor), to_f16(v[h].z, factor), to_f16(v[h].w, factor));
+        for (int h = 0; h < 2; ++h) {
+            uint32_t big = most_of(most[h]), small = least_of(least[h]);
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) { big = max(big, __shfl_xor_sync(0xffffffffu, big, o)); small = min(small, __shfl_xor_sync(0xffffffffu, small, o)); }
+            differ |= inexact(small) && (big >> 7) + 12u < exponent;
+            own[h] = factor_of(big);
+        }
+        if (__any_sync(0xffffffffu, differ)) {
+            half_to_f16(v[0], own[0]);
+            half_to_f16(v[1], own[1]);
+            return kOwn;
+        }
+    }
+    const int f = factor_of(m);
+    half_to_f16(v[0], f);
+    half_to_f16(v[1], f);
     return f;
 }
 
@@ -242,11 +286,16 @@ mx_stream_split_kernel(MxStream a)
     const int n = (int)(unit - chunk * (uint32_t)a.batch);
     const int64_t k = (int64_t)chunk * kChunk + lane * 8;
     uint4 v[2] = {load_x8(a, n, k), load_x8(a, n, k + 256)};
-    const int f = chunk_to_f16(v);
+    int own[2];
+    const int f = chunk_to_f16(v, own);
     uint8_t* to = a.x_chunks + (uint64_t)unit * kXPitch;
     *reinterpret_cast<uint4*>(to + lane * 16) = v[0];
     *reinterpret_cast<uint4*>(to + 512 + lane * 16) = v[1];
     if (lane == 0) *reinterpret_cast<int*>(to + 1024) = f;
+    if (f == kOwn && (lane & 3) == 0) {
+        reinterpret_cast<int8_t*>(to)[kXOwn + (lane >> 2)] = (int8_t)own[0];
+        reinterpret_cast<int8_t*>(to)[kXOwn + 8 + (lane >> 2)] = (int8_t)own[1];
+    }
 }
 
 // d * 2^h in two steps, for h that binary32 may not hold; NaN for the scale byte 255
@@ -334,11 +383,14 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                     for (int u = 0; u < kAhead; ++u) {
                         const int i = i0 + u * kXWarps;
                         if (i >= items) break;           // the same for the whole warp
-                        const int f = chunk_to_f16(v[u]);
+                        int own[2];
+                        const int f = chunk_to_f16(v[u], own);
                         const uint32_t to = at + x_at + i * kXPitch;
                         sts128(to + lane * 16u, v[u][0]);
                         sts128(to + 512u + lane * 16u, v[u][1]);
                         if (lane == 0) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + 1024u), "r"(f) : "memory");
+                        if (f == kOwn && (lane & 3) == 0)
+                            asm volatile("st.shared.s8 [%0], %1;\n st.shared.s8 [%0 + 8], %2;" ::"r"(to + kXOwn + (lane >> 2)), "r"(own[0]), "r"(own[1]) : "memory");
                     }
                 }
                 __syncwarp();
@@ -416,8 +468,12 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                                             part[n][0] += d[0] * __uint_as_float(sa); part[n][1] += d[1] * __uint_as_float(sa);
                                             part[n][2] += d[2] * __uint_as_float(sb); part[n][3] += d[3] * __uint_as_float(sb);
                                         } else {
-                                            part[n][0] += scale_far(d[0], sa >> 23, f[n][0]); part[n][1] += scale_far(d[1], sa >> 23, f[n][1]);
-                                            part[n][2] += scale_far(d[2], sb >> 23, f[n][0]); part[n][3] += scale_far(d[3], sb >> 23, f[n][1]);
+                                            int g[2];
+#pragma unroll
+                                            for (int c = 0; c < 2; ++c)
+                                                g[c] = f[n][c] != kOwn ? f[n][c] : lds_s8(at + x_at + (kg * a.batch + min(n * 8 + 2 * t + c, a.batch - 1)) * kXPitch + kXOwn + box * 8 + b + q);
+                                            part[n][0] += scale_far(d[0], sa >> 23, g[0]); part[n][1] += scale_far(d[1], sa >> 23, g[1]);
+                                            part[n][2] += scale_far(d[2], sb >> 23, g[0]); part[n][3] += scale_far(d[3], sb >> 23, g[1]);
                                         }
                                     }
                                 }
