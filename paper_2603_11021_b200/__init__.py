@@ -5,6 +5,9 @@ CUDA kernels of ``libllvq.so``.  PyTorch is used for device memory and streams.
 The calls that launch a product, a dequantization or an encoding go through the
 native module ``_native`` (``csrc/binding.cpp``), which checks the tensors and makes
 the output; load-time and multi-GPU calls go through ctypes.
+A call runs on ``stream``, or on PyTorch's current one; an output that it makes itself
+belongs to that stream, as if it had been made under ``torch.cuda.stream(stream)``, and
+is kept until what the current stream had been given by then is done with it.
 There is no CPU fallback: if the library is missing or the device is not a CUDA
 device, calls raise.
 """
@@ -187,6 +190,19 @@ def _out(call: str, r):
     return r
 
 
+def _new_bytes(nbytes: int, like: torch.Tensor, stream) -> torch.Tensor:
+    """An output of a call on ``stream``: PyTorch's allocator hands memory out per stream, before the work of its last owner there is done, so it
+    belongs to that stream; the current one, on which the caller reads it, is recorded where it is another."""
+    if stream is None or not like.is_cuda:
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    current = torch.cuda.current_stream(like.device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(int(stream.cuda_stream), device=like.device)):
+        t = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    if current.cuda_stream != int(stream.cuda_stream):
+        t.record_stream(current)
+    return t
+
+
 def _dev(t: torch.Tensor, name: str) -> int:
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous CUDA tensor")
@@ -315,7 +331,7 @@ def llvq_sort_blocks(ctx: Context, d_idx: torch.Tensor, n_out: int, k_in: int, d
     if nbytes == 0:
         raise LlvqError("llvq_sorted_bytes", 3)
     if d_sorted is None:
-        d_sorted = torch.empty(nbytes, dtype=torch.uint8, device=d_idx.device)
+        d_sorted = _new_bytes(nbytes, d_idx, stream)
     assert d_sorted.numel() * d_sorted.element_size() >= nbytes
     assert d_idx.numel() * d_idx.element_size() >= ctx.index_bytes(n_out * ((k_in + 23) // 24))
     _check("llvq_sort_blocks", ctx._lib.llvq_sort_blocks(ctx._h, _dev(d_idx, "d_idx"), n_out, k_in, _dev(d_sorted, "d_sorted"), _stream_ptr(stream)))
@@ -346,7 +362,7 @@ def llvq_sort_blocks_sg(ctx: Context, d_fields: torch.Tensor, gain_bits: int, n_
     if nbytes == 0:
         raise LlvqError("llvq_sorted_bytes", 3)
     if d_sorted is None:
-        d_sorted = torch.empty(nbytes, dtype=torch.uint8, device=d_fields.device)
+        d_sorted = _new_bytes(nbytes, d_fields, stream)
     assert d_sorted.numel() * d_sorted.element_size() >= nbytes
     assert d_fields.numel() * d_fields.element_size() >= int(ctx._lib.llvq_field_bytes(ctx._h, n_out * ((k_in + 23) // 24), gain_bits))
     _check("llvq_sort_blocks_sg", ctx._lib.llvq_sort_blocks_sg(ctx._h, _dev(d_fields, "d_fields"), gain_bits, n_out, k_in,
@@ -368,7 +384,7 @@ def llvq_sort_blocks_gemm(ctx: Context, d_idx: torch.Tensor, n_out: int, k_in: i
     if nbytes == 0:
         raise LlvqError("llvq_sorted_gemm_bytes", 3)
     if d_sorted is None:
-        d_sorted = torch.empty(nbytes, dtype=torch.uint8, device=d_idx.device)
+        d_sorted = _new_bytes(nbytes, d_idx, stream)
     assert d_sorted.numel() * d_sorted.element_size() >= nbytes
     assert d_idx.numel() * d_idx.element_size() >= ctx.index_bytes(n_out * ((k_in + 23) // 24))
     _check("llvq_sort_blocks_gemm", ctx._lib.llvq_sort_blocks_gemm(ctx._h, _dev(d_idx, "d_idx"), n_out, k_in, _dev(d_sorted, "d_sorted"),
@@ -389,7 +405,7 @@ def llvq_sort_blocks_gemm_sg(ctx: Context, d_fields: torch.Tensor, gain_bits: in
     if nbytes == 0:
         raise LlvqError("llvq_sorted_gemm_bytes", 3)
     if d_sorted is None:
-        d_sorted = torch.empty(nbytes, dtype=torch.uint8, device=d_fields.device)
+        d_sorted = _new_bytes(nbytes, d_fields, stream)
     assert d_sorted.numel() * d_sorted.element_size() >= nbytes
     _check("llvq_sort_blocks_gemm_sg", ctx._lib.llvq_sort_blocks_gemm_sg(ctx._h, _dev(d_fields, "d_fields"), gain_bits, n_out, k_in,
                                                                          _dev(d_sorted, "d_sorted"), _stream_ptr(stream)))

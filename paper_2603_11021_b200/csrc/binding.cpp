@@ -4,7 +4,7 @@
 // a call cost 12.8 us of host time, of which the launch itself is a quarter.
 //
 // Every function takes the context as the address in Context._ptr, tensors as they are, sizes as integers and the stream as a
-// CUDA stream address or None (PyTorch's current stream), and returns the output tensor, or a nonzero LLVQ status as an int
+// CUDA stream address or None (PyTorch's current stream of the first tensor's device), and returns the output tensor, or a nonzero LLVQ status as an int
 // for the caller to raise.  Violated expectations raise AssertionError, tensors of the wrong kind TypeError.
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -79,10 +79,30 @@ struct Args {
 
 uint64_t bytes_of(const at::Tensor& t) { return (uint64_t)t.numel() * (uint64_t)t.element_size(); }
 
-at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like)
+// The stream that the call is given, or PyTorch's current one of the device that `t` is on (a call on host memory has none: it is refused later).
+void* stream_of(Args& A, int i, const at::Tensor& t)
 {
-    if (like.is_cuda()) return at::detail::empty_cuda(shape, type, like.device(), std::nullopt);       // past the dispatcher: half a microsecond less
-    return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    if (!A.ok) return nullptr;
+    if (A.a[i] != Py_None) return A.stream(i);
+    return t.is_cuda() ? c10::cuda::getCurrentCUDAStream(t.device().index()).stream() : nullptr;
+}
+
+at::Tensor empty_cuda(at::IntArrayRef shape, at::ScalarType type, at::Device device)
+{
+    return at::detail::empty_cuda(shape, type, device, std::nullopt);       // past the dispatcher: half a microsecond less
+}
+
+// An output of a call on `stream`, on the device of `like`.  PyTorch's allocator hands memory out per stream, before the work of its last owner there is
+// done: an output belongs to the stream of the kernel that writes it.  The caller reads it on the current one, which is recorded where it is another.
+at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like, void* stream)
+{
+    if (!like.is_cuda()) return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(like.device().index());
+    if (current.stream() == stream) return empty_cuda(shape, type, like.device());
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
+    at::Tensor t = empty_cuda(shape, type, like.device());
+    c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+    return t;
 }
 
 // the output tensor, or the status
@@ -130,7 +150,9 @@ LLVQ_FUNC(gemv, 10)
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(7);
     const bool sorted = A.a[9] == Py_True;
     if (!A.ok) return nullptr;
-    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w);
+    void* st = stream_of(A, 8, *w);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in && g->scalar_type() == at::kHalf);
     A.expect((y.scalar_type() == at::kFloat || y.scalar_type() == at::kBFloat16) && y.numel() >= n_out);
     const uint64_t nblocks = blocks_of(n_out, k_in);
@@ -138,7 +160,6 @@ LLVQ_FUNC(gemv, 10)
     const void* pw = A.device(w, sorted ? "d_sorted" : "d_idx");
     const uint16_t *pg = static_cast<const uint16_t*>(A.device(g, "d_gain")), *px = static_cast<const uint16_t*>(A.device(x, "d_x"));
     void* py = A.device(&y, "d_y");
-    void* st = A.stream(8);
     if (!A.ok) return nullptr;
     const int s = call([&] {
         return sorted ? llvq_gemv_sorted(ctx, pw, pg, n_out, k_in, px, py, y_code(y.scalar_type()), st)
@@ -166,7 +187,9 @@ LLVQ_FUNC(gemv_sg, 12)
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(9);
     const bool sorted = A.a[11] == Py_True;
     if (!A.ok) return nullptr;
-    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w);
+    void* st = stream_of(A, 10, *w);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in);
     A.expect((y.scalar_type() == at::kFloat || y.scalar_type() == at::kBFloat16) && y.numel() >= n_out);
     if (!A.ok) return nullptr;
@@ -175,7 +198,6 @@ LLVQ_FUNC(gemv_sg, 12)
     const void* pw = A.device(w, sorted ? "d_sorted" : "d_fields");
     const uint16_t* px = static_cast<const uint16_t*>(A.device(x, "d_x"));
     void* py = A.device(&y, "d_y");
-    void* st = A.stream(10);
     if (!A.ok) return nullptr;
     const int s = call([&] {
         return sorted ? llvq_gemv_sorted_sg(ctx, pw, (int)bits, p.cb, p.rs, n_out, k_in, px, py, y_code(y.scalar_type()), st)
@@ -195,7 +217,9 @@ LLVQ_FUNC(gemm, 9)
     if (!A.expect(x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in && g->scalar_type() == at::kHalf)) return nullptr;
     const int64_t batch = x->size(0);
     if (!A.expect(form != 2 || y0)) return nullptr;             // that call allocates nothing: Y has to be passed in
-    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w);
+    void* st = stream_of(A, 7, *w);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w, st);
     A.expect(y.scalar_type() == at::kBFloat16 && y.numel() >= batch * n_out);
     const uint64_t nblocks = blocks_of(n_out, k_in);
     A.expect(form == 2 || ((uint64_t)g->numel() >= nblocks &&
@@ -203,7 +227,6 @@ LLVQ_FUNC(gemm, 9)
     const void* pw = A.device(w, form == 1 ? "d_sorted" : "d_idx");
     const uint16_t *pg = static_cast<const uint16_t*>(A.device(g, "d_gain")), *px = static_cast<const uint16_t*>(A.device(x, "d_x"));
     uint16_t* py = static_cast<uint16_t*>(A.device(&y, "d_y"));
-    void* st = A.stream(7);
     if (!A.ok) return nullptr;
     const int s = call([&] {
         return form == 1   ? llvq_gemm_small_batch_sorted(ctx, pw, pg, n_out, k_in, px, (int)batch, py, st)
@@ -224,14 +247,15 @@ LLVQ_FUNC(gemm_sg, 11)
     if (!A.ok) return nullptr;
     if (!A.expect(x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in)) return nullptr;
     const int64_t batch = x->size(0);
-    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w);
+    void* st = stream_of(A, 9, *w);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w, st);
     if (!A.expect(y.scalar_type() == at::kBFloat16 && y.numel() >= batch * n_out)) return nullptr;
     const SgPtrs p = sg_args(A, cb, rs, bits, n_out);
     A.expect(bytes_of(*w) >= (sorted ? llvq_sorted_gemm_bytes(ctx, n_out, k_in) : llvq_field_bytes(ctx, blocks_of(n_out, k_in), (int)bits)));
     const void* pw = A.device(w, sorted ? "d_sorted" : "d_fields");
     const uint16_t* px = static_cast<const uint16_t*>(A.device(x, "d_x"));
     uint16_t* py = static_cast<uint16_t*>(A.device(&y, "d_y"));
-    void* st = A.stream(9);
     if (!A.ok) return nullptr;
     const int s = call([&] {
         return sorted ? llvq_gemm_small_batch_sorted_sg(ctx, pw, (int)bits, p.cb, p.rs, n_out, k_in, px, (int)batch, py, st)
@@ -292,7 +316,9 @@ LLVQ_FUNC(dequant, 9)
     const at::Tensor *idx = A.tensor(1, "d_idx"), *g = A.tensor(2, "d_gain"), *w0 = A.tensor_or_none(6, "d_w");
     const int64_t rows = A.integer(3), cols = A.integer(4), layout = A.integer(5), ld = A.integer(7);
     if (!A.ok) return nullptr;
-    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *idx);
+    void* st = stream_of(A, 8, *idx);
+    if (!A.ok) return nullptr;
+    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *idx, st);
     A.expect(w.scalar_type() == at::kBFloat16 && g->scalar_type() == at::kHalf);
     const uint64_t nblocks = layout == LLVQ_LAYOUT_FLAT ? ((uint64_t)rows * (uint64_t)cols + 23) / 24 : blocks_of(rows, cols);
     A.expect((uint64_t)g->numel() >= nblocks && bytes_of(*idx) >= llvq_index_bytes(ctx, nblocks));
@@ -300,7 +326,6 @@ LLVQ_FUNC(dequant, 9)
     const void* pi = A.device(idx, "d_idx");
     const uint16_t* pg = static_cast<const uint16_t*>(A.device(g, "d_gain"));
     uint16_t* pw = static_cast<uint16_t*>(A.device(&w, "d_w"));
-    void* st = A.stream(8);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_dequant_matrix(ctx, pi, pg, rows, cols, (int)layout, pw, ld, st); });
     return result(s, std::move(w));
@@ -313,14 +338,15 @@ LLVQ_FUNC(dequant_sg, 10)
     const at::Tensor *f = A.tensor(1, "d_fields"), *cb = A.tensor(3, "d_codebook"), *rs = A.tensor_or_none(4, "d_row_scale"), *w0 = A.tensor_or_none(7, "d_w");
     const int64_t bits = A.integer(2), rows = A.integer(5), cols = A.integer(6), ld = A.integer(8);
     if (!A.ok) return nullptr;
-    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *f);
+    void* st = stream_of(A, 9, *f);
+    if (!A.ok) return nullptr;
+    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *f, st);
     A.expect(w.scalar_type() == at::kBFloat16);
     if (!A.expect(holds(w, rows, cols, ld))) return nullptr;
     const SgPtrs p = sg_args(A, cb, rs, bits, rows);
     A.expect(bytes_of(*f) >= llvq_field_bytes(ctx, blocks_of(rows, cols), (int)bits));
     const void* pf = A.device(f, "d_fields");
     uint16_t* pw = static_cast<uint16_t*>(A.device(&w, "d_w"));
-    void* st = A.stream(9);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_dequant_matrix_sg(ctx, pf, (int)bits, p.cb, p.rs, rows, cols, pw, ld, st); });
     return result(s, std::move(w));
@@ -333,12 +359,13 @@ LLVQ_FUNC(decode, 5)
     const at::Tensor *idx = A.tensor(1, "d_idx"), *p0 = A.tensor_or_none(3, "d_points");
     const int64_t n = A.integer(2);
     if (!A.ok) return nullptr;
-    at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *idx);
+    void* st = stream_of(A, 4, *idx);
+    if (!A.ok) return nullptr;
+    at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *idx, st);
     A.expect(p.scalar_type() == at::kChar && p.numel() >= n * 24);
     A.expect(bytes_of(*idx) >= llvq_index_bytes(ctx, (uint64_t)n));
     const void* pi = A.device(idx, "d_idx");
     int8_t* pp = static_cast<int8_t*>(A.device(&p, "d_points"));
-    void* st = A.stream(4);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_decode_blocks(ctx, pi, (uint64_t)n, pp, st); });
     return result(s, std::move(p));
@@ -353,12 +380,13 @@ LLVQ_FUNC(encode, 6)
     if (!A.ok) return nullptr;
     if (!A.expect(v->scalar_type() == at::kFloat && v->dim() == 2 && v->size(1) == 24)) return nullptr;
     const int64_t n = v->size(0);
-    at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *v), ix = i0 ? *i0 : new_tensor({n}, at::kLong, *v);
+    void* st = stream_of(A, 5, *v);
+    if (!A.ok) return nullptr;
+    at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *v, st), ix = i0 ? *i0 : new_tensor({n}, at::kLong, *v, st);
     A.expect(p.scalar_type() == at::kChar && p.numel() >= n * 24 && ix.scalar_type() == at::kLong && ix.numel() >= n);
     const float* pv = static_cast<const float*>(A.device(v, "d_v"));
     int8_t* pp = static_cast<int8_t*>(A.device(&p, "d_points"));
     uint64_t* pi = static_cast<uint64_t*>(A.device(&ix, "d_index"));
-    void* st = A.stream(5);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_encode_blocks(ctx, pv, (uint64_t)n, (int)metric, pp, pi, st); });
     if (s != LLVQ_OK) return PyLong_FromLong(s);
@@ -378,11 +406,12 @@ LLVQ_FUNC(rank, 4)
     if (!A.ok) return nullptr;
     if (!A.expect(p->scalar_type() == at::kChar && p->dim() == 2 && p->size(1) == 24)) return nullptr;
     const int64_t n = p->size(0);
-    at::Tensor ix = i0 ? *i0 : new_tensor({n}, at::kLong, *p);
+    void* st = stream_of(A, 3, *p);
+    if (!A.ok) return nullptr;
+    at::Tensor ix = i0 ? *i0 : new_tensor({n}, at::kLong, *p, st);
     A.expect(ix.scalar_type() == at::kLong && ix.numel() >= n);
     const int8_t* pp = static_cast<const int8_t*>(A.device(p, "d_points"));
     uint64_t* pi = static_cast<uint64_t*>(A.device(&ix, "d_index"));
-    void* st = A.stream(3);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_rank_blocks(ctx, pp, (uint64_t)n, pi, st); });
     return result(s, std::move(ix));
@@ -398,27 +427,20 @@ LLVQ_FUNC(pack, 6)
     if (!A.expect(ix->scalar_type() == at::kLong)) return nullptr;
     const int64_t n = ix->numel();
     const uint64_t nbytes = llvq_field_bytes(ctx, (uint64_t)n, (int)bits);
-    at::Tensor f = f0 ? *f0 : new_tensor({(int64_t)nbytes}, at::kByte, *ix);
+    void* st = stream_of(A, 5, *ix);
+    if (!A.ok) return nullptr;
+    at::Tensor f = f0 ? *f0 : new_tensor({(int64_t)nbytes}, at::kByte, *ix, st);
     A.expect(bytes_of(f) >= nbytes);
     A.expect(bits == 0 || (k && k->scalar_type() == at::kByte && k->numel() >= n));
     const uint64_t* pi = static_cast<const uint64_t*>(A.device(ix, "d_index"));
     const uint8_t* pk = bits == 0 ? nullptr : static_cast<const uint8_t*>(A.device(k, "d_gain_index"));
     void* pf = A.device(&f, "d_fields");
-    void* st = A.stream(5);
     if (!A.ok) return nullptr;
     const int s = call([&] { return llvq_pack_fields(ctx, pi, pk, (int)bits, (uint64_t)n, pf, st); });
     return result(s, std::move(f));
 }
 
 // ---- microscaled 4-bit floating point, embedding tables --------------------------------------------------------------------------
-
-// The stream that the call is given, or PyTorch's current one of the device that `t` is on.
-void* stream_of(Args& A, int i, const at::Tensor& t)
-{
-    if (!A.ok) return nullptr;
-    if (A.a[i] == Py_None && t.is_cuda()) return c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
-    return A.stream(i);
-}
 
 // The tensor's memory, on the context's device.
 void* on_device(Args& A, const llvq_ctx* ctx, const at::Tensor* t, const char* name)
@@ -497,9 +519,10 @@ LLVQ_FUNC(mx_quantize, 5)
     if (!x->is_cuda()) { A.wrong("d_x"); return nullptr; }
     if (!A.expect((cols <= 1 || x->stride(1) == 1) && ld >= cols)) return nullptr;
     if (llvq_device(ctx) >= 0 && !A.expect(x->device().index() == llvq_device(ctx))) return nullptr;
-    at::Tensor c = c0 ? *c0 : new_tensor({rows, llvq_mx_code_pitch(cols)}, at::kByte, *x), s = s0 ? *s0 : new_tensor({rows, llvq_mx_scale_pitch(cols)}, at::kByte, *x);
-    const Mx m = mx_args(A, ctx, &c, &s, rows, cols);
     void* st = stream_of(A, 4, *x);
+    if (!A.ok) return nullptr;
+    at::Tensor c = c0 ? *c0 : new_tensor({rows, llvq_mx_code_pitch(cols)}, at::kByte, *x, st), s = s0 ? *s0 : new_tensor({rows, llvq_mx_scale_pitch(cols)}, at::kByte, *x, st);
+    const Mx m = mx_args(A, ctx, &c, &s, rows, cols);
     if (!A.ok) return nullptr;
     const void* px = x->data_ptr();
     const int r = call([&] { return llvq_mx_quantize(ctx, px, type, rows, cols, ld, const_cast<uint8_t*>(m.codes), const_cast<uint8_t*>(m.scales), st); });
@@ -515,13 +538,14 @@ LLVQ_FUNC(mx_dequant, 8)
     const int64_t rows = A.integer(3), cols = A.integer(4), ld = A.integer(6);
     if (!A.ok) return nullptr;
     if (!A.expect(rows >= 0 && cols >= 0 && ld >= cols)) return nullptr;
-    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *c);
+    void* st = stream_of(A, 7, *c);
+    if (!A.ok) return nullptr;
+    at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *c, st);
     A.expect(w.scalar_type() == at::kBFloat16);
     A.expect(holds(w, rows, cols, ld));
     if (!A.ok) return nullptr;
     const Mx m = mx_args(A, ctx, c, s, rows, cols);
     uint16_t* pw = static_cast<uint16_t*>(on_device(A, ctx, &w, "d_w"));
-    void* st = stream_of(A, 7, *c);
     if (!A.ok) return nullptr;
     const int r = call([&] { return llvq_mx_dequant_matrix(ctx, m.codes, m.scales, rows, cols, pw, ld, st); });
     return result(r, std::move(w));
@@ -536,12 +560,14 @@ LLVQ_FUNC(mx_gemv, 9)
     if (!A.ok) return nullptr;
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(7);
     if (!A.expect(n_out >= 0 && (yt == at::kFloat || yt == at::kBFloat16))) return nullptr;
-    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *c);
+    void* st = stream_of(A, 8, *c);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *c, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in && y.numel() >= n_out);
     if (!A.ok) return nullptr;
     const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
     const uint16_t* px = static_cast<const uint16_t*>(on_device(A, ctx, x, "d_x"));
-    void *py = on_device(A, ctx, &y, "d_y"), *st = stream_of(A, 8, *c);
+    void* py = on_device(A, ctx, &y, "d_y");
     if (!A.ok) return nullptr;
     const int r = call([&] { return llvq_mx_gemv(ctx, m.codes, m.scales, n_out, k_in, px, py, y_code(yt), st); });
     return result(r, std::move(y));
@@ -557,13 +583,14 @@ LLVQ_FUNC(mx_gemm_small, 8)
     if (!A.expect(n_out >= 0 && x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in)) return nullptr;
     const int64_t batch = x->size(0);
     if (batch > 64) return PyLong_FromLong(LLVQ_EUNSUPPORTED);
-    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *c);
+    void* st = stream_of(A, 7, *c);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *c, st);
     A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)batch * n_out);
     if (!A.ok) return nullptr;
     const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
     const uint16_t* px = static_cast<const uint16_t*>(on_device(A, ctx, x, "d_x"));
     uint16_t* py = static_cast<uint16_t*>(on_device(A, ctx, &y, "d_y"));
-    void* st = stream_of(A, 7, *c);
     if (!A.ok) return nullptr;
     const Workspace work(llvq_mx_small_batch_bytes(ctx, n_out, k_in, (int)batch), *c, st);
     const int r = call([&] { return llvq_mx_gemm_small_batch(ctx, m.codes, m.scales, n_out, k_in, px, (int)batch, py, work.p, st); });
@@ -579,24 +606,25 @@ LLVQ_FUNC(mx_gemm, 10)
     const int64_t tokens = A.integer(3), n_out = A.integer(6), k_in = A.integer(7);
     if (!A.ok) return nullptr;
     if (!A.expect(mx_holds(*xc, *xs, tokens, k_in) && mx_holds(*c, *s, n_out, k_in))) return nullptr;
-    at::Tensor y = y0 ? *y0 : new_tensor({tokens, n_out}, at::kBFloat16, *c);
+    void* st = stream_of(A, 9, *c);
+    if (!A.ok) return nullptr;
+    at::Tensor y = y0 ? *y0 : new_tensor({tokens, n_out}, at::kBFloat16, *c, st);
     A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)tokens * n_out);
     if (!A.ok) return nullptr;
     const Mx x = mx_args(A, ctx, xc, xs, tokens, k_in);
     if (!A.ok) return nullptr;
     const Mx m = mx_args(A, ctx, c, s, n_out, k_in);
     uint16_t* py = static_cast<uint16_t*>(on_device(A, ctx, &y, "d_y"));
-    void* st = stream_of(A, 9, *c);
     if (!A.ok) return nullptr;
     const int r = call([&] { return llvq_mx_gemm(ctx, x.codes, x.scales, tokens, m.codes, m.scales, n_out, k_in, py, st); });
     return result(r, std::move(y));
 }
 
-at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type)
+at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type, void* stream)
 {
     std::vector<int64_t> shape(tokens.sizes().begin(), tokens.sizes().end());
     shape.push_back(dim);
-    return new_tensor(shape, type, tokens);
+    return new_tensor(shape, type, tokens, stream);
 }
 
 // (ctx, table, tokens, scale, out or None, stream)
@@ -609,11 +637,13 @@ LLVQ_FUNC(embed, 6)
     const int type = float_code(w->scalar_type());
     if (!A.expect(type >= 0 && w->dim() == 2)) return nullptr;
     const int64_t n = t->numel(), dim = w->size(1);
-    at::Tensor o = o0 ? *o0 : embedded(*t, dim, w->scalar_type());
+    void* st = stream_of(A, 5, *w);
+    if (!A.ok) return nullptr;
+    at::Tensor o = o0 ? *o0 : embedded(*t, dim, w->scalar_type(), st);
     if (!A.expect(o.scalar_type() == w->scalar_type() && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
     int bytes;
     const void *pt = token_args(A, ctx, t, &bytes), *pw = on_device(A, ctx, w, "d_table");
-    void *po = on_device(A, ctx, &o, "d_out"), *st = stream_of(A, 5, *w);
+    void* po = on_device(A, ctx, &o, "d_out");
     if (!A.ok) return nullptr;
     const int r = call([&] { return llvq_embed(ctx, pw, type, w->size(0), dim, pt, bytes, n, (float)scale, po, st); });
     return result(r, std::move(o));
@@ -629,14 +659,15 @@ LLVQ_FUNC(mx_embed, 9)
     if (!A.ok) return nullptr;
     if (!A.expect(dim >= 0)) return nullptr;
     const int64_t n = t->numel();
-    at::Tensor o = o0 ? *o0 : embedded(*t, dim, at::kBFloat16);
+    void* st = stream_of(A, 8, *c);
+    if (!A.ok) return nullptr;
+    at::Tensor o = o0 ? *o0 : embedded(*t, dim, at::kBFloat16, st);
     if (!A.expect(o.scalar_type() == at::kBFloat16 && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
     const Mx m = mx_args(A, ctx, c, s, vocab, dim);
     if (!A.ok) return nullptr;
     int bytes;
     const void* pt = token_args(A, ctx, t, &bytes);
     uint16_t* po = static_cast<uint16_t*>(on_device(A, ctx, &o, "d_out"));
-    void* st = stream_of(A, 8, *c);
     if (!A.ok) return nullptr;
     const int r = call([&] { return llvq_mx_embed(ctx, m.codes, m.scales, vocab, dim, pt, bytes, n, (float)scale, po, st); });
     return result(r, std::move(o));
@@ -657,11 +688,13 @@ LLVQ_FUNC(embed_grad, 10)
     if (!A.expect(type >= 0 && grad_type >= 0 && vocab >= 0 && dy->dim() >= 1 && (!accumulate || g0))) return nullptr;
     const int64_t n = t->numel(), dim = dy->size(-1);
     if (!A.expect((__int128)dy->numel() == (__int128)n * dim)) return nullptr;
-    at::Tensor g = g0 ? *g0 : new_tensor({vocab, dim}, gt, *dy);
+    void* st = stream_of(A, 9, *dy);
+    if (!A.ok) return nullptr;
+    at::Tensor g = g0 ? *g0 : new_tensor({vocab, dim}, gt, *dy, st);
     if (!A.expect((__int128)g.numel() >= (__int128)vocab * dim)) return nullptr;
     int bytes;
     const void *pt = token_args(A, ctx, t, &bytes), *pd = on_device(A, ctx, dy, "d_dy");
-    void *pg = on_device(A, ctx, &g, "d_grad"), *st = stream_of(A, 9, *dy);
+    void* pg = on_device(A, ctx, &g, "d_grad");
     if (!A.ok) return nullptr;
     const Workspace work(llvq_embed_grad_bytes(n, dim), *dy, st);
     const int r = call([&] {
