@@ -6,8 +6,8 @@ The calls that launch a product, a dequantization or an encoding go through the
 native module ``_native`` (``csrc/binding.cpp``), which checks the tensors and makes
 the output; load-time and multi-GPU calls go through ctypes.
 A call runs on ``stream``, or on PyTorch's current one; an output that it makes itself
-belongs to that stream, as if it had been made under ``torch.cuda.stream(stream)``, and
-is kept until what the current stream had been given by then is done with it.
+belongs to that stream, as if it had been made under ``torch.cuda.stream(stream)``; its
+memory, once dropped, is not used again before the current stream is done with it too.
 There is no CPU fallback: if the library is missing or the device is not a CUDA
 device, calls raise.
 """

@@ -10,8 +10,11 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/Context.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/record_function.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -80,27 +83,44 @@ struct Args {
 uint64_t bytes_of(const at::Tensor& t) { return (uint64_t)t.numel() * (uint64_t)t.element_size(); }
 
 // The stream that the call is given, or PyTorch's current one of the device that `t` is on (a call on host memory has none: it is refused later).
-void* stream_of(Args& A, int i, const at::Tensor& t)
+struct CallStream {
+    void* p = nullptr;
+    bool current = true;
+    mutable int watched = -1;           // whether outputs are made through the dispatcher; -1: not looked yet
+    operator void*() const { return p; }
+};
+CallStream stream_of(Args& A, int i, const at::Tensor& t)
 {
-    if (!A.ok) return nullptr;
-    if (A.a[i] != Py_None) return A.stream(i);
-    return t.is_cuda() ? c10::cuda::getCurrentCUDAStream(t.device().index()).stream() : nullptr;
+    CallStream s;
+    if (A.a[i] != Py_None) s.p = A.stream(i);
+    if (!A.ok || !t.is_cuda()) return s;
+    void* const current = c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
+    if (A.a[i] == Py_None) s.p = current;
+    s.current = s.p == current;
+    return s;
 }
 
-at::Tensor empty_cuda(at::IntArrayRef shape, at::ScalarType type, at::Device device)
+// Past the dispatcher, for half a microsecond less, unless somebody behind it wants to know: a dispatch mode, a profiler, or
+// torch.utils.deterministic.fill_uninitialized_memory.
+at::Tensor empty_cuda(at::IntArrayRef shape, at::ScalarType type, at::Device device, const CallStream& stream)
 {
-    return at::detail::empty_cuda(shape, type, device, std::nullopt);       // past the dispatcher: half a microsecond less
+    if (stream.watched < 0) {
+        const at::Context& c = at::globalContext();
+        stream.watched = c10::impl::TorchDispatchModeTLS::any_modes_set() || at::hasCallbacks() || (c.deterministicAlgorithms() && c.deterministicFillUninitializedMemory());
+    }
+    if (stream.watched) return at::empty(shape, at::TensorOptions().dtype(type).device(device));
+    return at::detail::empty_cuda(shape, type, device, std::nullopt);
 }
 
 // An output of a call on `stream`, on the device of `like`.  PyTorch's allocator hands memory out per stream, before the work of its last owner there is
 // done: an output belongs to the stream of the kernel that writes it.  The caller reads it on the current one, which is recorded where it is another.
-at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like, void* stream)
+at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like, const CallStream& stream)
 {
     if (!like.is_cuda()) return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+    if (stream.current) return empty_cuda(shape, type, like.device(), stream);
     const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(like.device().index());
-    if (current.stream() == stream) return empty_cuda(shape, type, like.device());
-    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), like.device().index()));
-    at::Tensor t = empty_cuda(shape, type, like.device());
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream.p), like.device().index()));
+    at::Tensor t = empty_cuda(shape, type, like.device(), stream);
     c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
     return t;
 }
@@ -150,7 +170,7 @@ LLVQ_FUNC(gemv, 10)
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(7);
     const bool sorted = A.a[9] == Py_True;
     if (!A.ok) return nullptr;
-    void* st = stream_of(A, 8, *w);
+    const CallStream st = stream_of(A, 8, *w);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in && g->scalar_type() == at::kHalf);
@@ -187,7 +207,7 @@ LLVQ_FUNC(gemv_sg, 12)
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(9);
     const bool sorted = A.a[11] == Py_True;
     if (!A.ok) return nullptr;
-    void* st = stream_of(A, 10, *w);
+    const CallStream st = stream_of(A, 10, *w);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *w, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in);
@@ -217,7 +237,7 @@ LLVQ_FUNC(gemm, 9)
     if (!A.expect(x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in && g->scalar_type() == at::kHalf)) return nullptr;
     const int64_t batch = x->size(0);
     if (!A.expect(form != 2 || y0)) return nullptr;             // that call allocates nothing: Y has to be passed in
-    void* st = stream_of(A, 7, *w);
+    const CallStream st = stream_of(A, 7, *w);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w, st);
     A.expect(y.scalar_type() == at::kBFloat16 && y.numel() >= batch * n_out);
@@ -247,7 +267,7 @@ LLVQ_FUNC(gemm_sg, 11)
     if (!A.ok) return nullptr;
     if (!A.expect(x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in)) return nullptr;
     const int64_t batch = x->size(0);
-    void* st = stream_of(A, 9, *w);
+    const CallStream st = stream_of(A, 9, *w);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *w, st);
     if (!A.expect(y.scalar_type() == at::kBFloat16 && y.numel() >= batch * n_out)) return nullptr;
@@ -316,7 +336,7 @@ LLVQ_FUNC(dequant, 9)
     const at::Tensor *idx = A.tensor(1, "d_idx"), *g = A.tensor(2, "d_gain"), *w0 = A.tensor_or_none(6, "d_w");
     const int64_t rows = A.integer(3), cols = A.integer(4), layout = A.integer(5), ld = A.integer(7);
     if (!A.ok) return nullptr;
-    void* st = stream_of(A, 8, *idx);
+    const CallStream st = stream_of(A, 8, *idx);
     if (!A.ok) return nullptr;
     at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *idx, st);
     A.expect(w.scalar_type() == at::kBFloat16 && g->scalar_type() == at::kHalf);
@@ -338,7 +358,7 @@ LLVQ_FUNC(dequant_sg, 10)
     const at::Tensor *f = A.tensor(1, "d_fields"), *cb = A.tensor(3, "d_codebook"), *rs = A.tensor_or_none(4, "d_row_scale"), *w0 = A.tensor_or_none(7, "d_w");
     const int64_t bits = A.integer(2), rows = A.integer(5), cols = A.integer(6), ld = A.integer(8);
     if (!A.ok) return nullptr;
-    void* st = stream_of(A, 9, *f);
+    const CallStream st = stream_of(A, 9, *f);
     if (!A.ok) return nullptr;
     at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *f, st);
     A.expect(w.scalar_type() == at::kBFloat16);
@@ -359,7 +379,7 @@ LLVQ_FUNC(decode, 5)
     const at::Tensor *idx = A.tensor(1, "d_idx"), *p0 = A.tensor_or_none(3, "d_points");
     const int64_t n = A.integer(2);
     if (!A.ok) return nullptr;
-    void* st = stream_of(A, 4, *idx);
+    const CallStream st = stream_of(A, 4, *idx);
     if (!A.ok) return nullptr;
     at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *idx, st);
     A.expect(p.scalar_type() == at::kChar && p.numel() >= n * 24);
@@ -380,7 +400,7 @@ LLVQ_FUNC(encode, 6)
     if (!A.ok) return nullptr;
     if (!A.expect(v->scalar_type() == at::kFloat && v->dim() == 2 && v->size(1) == 24)) return nullptr;
     const int64_t n = v->size(0);
-    void* st = stream_of(A, 5, *v);
+    const CallStream st = stream_of(A, 5, *v);
     if (!A.ok) return nullptr;
     at::Tensor p = p0 ? *p0 : new_tensor({n, 24}, at::kChar, *v, st), ix = i0 ? *i0 : new_tensor({n}, at::kLong, *v, st);
     A.expect(p.scalar_type() == at::kChar && p.numel() >= n * 24 && ix.scalar_type() == at::kLong && ix.numel() >= n);
@@ -406,7 +426,7 @@ LLVQ_FUNC(rank, 4)
     if (!A.ok) return nullptr;
     if (!A.expect(p->scalar_type() == at::kChar && p->dim() == 2 && p->size(1) == 24)) return nullptr;
     const int64_t n = p->size(0);
-    void* st = stream_of(A, 3, *p);
+    const CallStream st = stream_of(A, 3, *p);
     if (!A.ok) return nullptr;
     at::Tensor ix = i0 ? *i0 : new_tensor({n}, at::kLong, *p, st);
     A.expect(ix.scalar_type() == at::kLong && ix.numel() >= n);
@@ -427,7 +447,7 @@ LLVQ_FUNC(pack, 6)
     if (!A.expect(ix->scalar_type() == at::kLong)) return nullptr;
     const int64_t n = ix->numel();
     const uint64_t nbytes = llvq_field_bytes(ctx, (uint64_t)n, (int)bits);
-    void* st = stream_of(A, 5, *ix);
+    const CallStream st = stream_of(A, 5, *ix);
     if (!A.ok) return nullptr;
     at::Tensor f = f0 ? *f0 : new_tensor({(int64_t)nbytes}, at::kByte, *ix, st);
     A.expect(bytes_of(f) >= nbytes);
@@ -519,7 +539,7 @@ LLVQ_FUNC(mx_quantize, 5)
     if (!x->is_cuda()) { A.wrong("d_x"); return nullptr; }
     if (!A.expect((cols <= 1 || x->stride(1) == 1) && ld >= cols)) return nullptr;
     if (llvq_device(ctx) >= 0 && !A.expect(x->device().index() == llvq_device(ctx))) return nullptr;
-    void* st = stream_of(A, 4, *x);
+    const CallStream st = stream_of(A, 4, *x);
     if (!A.ok) return nullptr;
     at::Tensor c = c0 ? *c0 : new_tensor({rows, llvq_mx_code_pitch(cols)}, at::kByte, *x, st), s = s0 ? *s0 : new_tensor({rows, llvq_mx_scale_pitch(cols)}, at::kByte, *x, st);
     const Mx m = mx_args(A, ctx, &c, &s, rows, cols);
@@ -538,7 +558,7 @@ LLVQ_FUNC(mx_dequant, 8)
     const int64_t rows = A.integer(3), cols = A.integer(4), ld = A.integer(6);
     if (!A.ok) return nullptr;
     if (!A.expect(rows >= 0 && cols >= 0 && ld >= cols)) return nullptr;
-    void* st = stream_of(A, 7, *c);
+    const CallStream st = stream_of(A, 7, *c);
     if (!A.ok) return nullptr;
     at::Tensor w = w0 ? *w0 : new_tensor({rows, ld}, at::kBFloat16, *c, st);
     A.expect(w.scalar_type() == at::kBFloat16);
@@ -560,7 +580,7 @@ LLVQ_FUNC(mx_gemv, 9)
     if (!A.ok) return nullptr;
     const at::ScalarType yt = y0 ? y0->scalar_type() : A.dtype(7);
     if (!A.expect(n_out >= 0 && (yt == at::kFloat || yt == at::kBFloat16))) return nullptr;
-    void* st = stream_of(A, 8, *c);
+    const CallStream st = stream_of(A, 8, *c);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({n_out}, yt, *c, st);
     A.expect(x->scalar_type() == at::kBFloat16 && x->numel() >= k_in && y.numel() >= n_out);
@@ -583,7 +603,7 @@ LLVQ_FUNC(mx_gemm_small, 8)
     if (!A.expect(n_out >= 0 && x->scalar_type() == at::kBFloat16 && x->dim() == 2 && x->size(1) == k_in)) return nullptr;
     const int64_t batch = x->size(0);
     if (batch > 64) return PyLong_FromLong(LLVQ_EUNSUPPORTED);
-    void* st = stream_of(A, 7, *c);
+    const CallStream st = stream_of(A, 7, *c);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({batch, n_out}, at::kBFloat16, *c, st);
     A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)batch * n_out);
@@ -606,7 +626,7 @@ LLVQ_FUNC(mx_gemm, 10)
     const int64_t tokens = A.integer(3), n_out = A.integer(6), k_in = A.integer(7);
     if (!A.ok) return nullptr;
     if (!A.expect(mx_holds(*xc, *xs, tokens, k_in) && mx_holds(*c, *s, n_out, k_in))) return nullptr;
-    void* st = stream_of(A, 9, *c);
+    const CallStream st = stream_of(A, 9, *c);
     if (!A.ok) return nullptr;
     at::Tensor y = y0 ? *y0 : new_tensor({tokens, n_out}, at::kBFloat16, *c, st);
     A.expect(y.scalar_type() == at::kBFloat16 && (__int128)y.numel() >= (__int128)tokens * n_out);
@@ -620,7 +640,7 @@ LLVQ_FUNC(mx_gemm, 10)
     return result(r, std::move(y));
 }
 
-at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type, void* stream)
+at::Tensor embedded(const at::Tensor& tokens, int64_t dim, at::ScalarType type, const CallStream& stream)
 {
     std::vector<int64_t> shape(tokens.sizes().begin(), tokens.sizes().end());
     shape.push_back(dim);
@@ -637,7 +657,7 @@ LLVQ_FUNC(embed, 6)
     const int type = float_code(w->scalar_type());
     if (!A.expect(type >= 0 && w->dim() == 2)) return nullptr;
     const int64_t n = t->numel(), dim = w->size(1);
-    void* st = stream_of(A, 5, *w);
+    const CallStream st = stream_of(A, 5, *w);
     if (!A.ok) return nullptr;
     at::Tensor o = o0 ? *o0 : embedded(*t, dim, w->scalar_type(), st);
     if (!A.expect(o.scalar_type() == w->scalar_type() && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
@@ -659,7 +679,7 @@ LLVQ_FUNC(mx_embed, 9)
     if (!A.ok) return nullptr;
     if (!A.expect(dim >= 0)) return nullptr;
     const int64_t n = t->numel();
-    void* st = stream_of(A, 8, *c);
+    const CallStream st = stream_of(A, 8, *c);
     if (!A.ok) return nullptr;
     at::Tensor o = o0 ? *o0 : embedded(*t, dim, at::kBFloat16, st);
     if (!A.expect(o.scalar_type() == at::kBFloat16 && (__int128)o.numel() >= (__int128)n * dim)) return nullptr;
@@ -688,7 +708,7 @@ LLVQ_FUNC(embed_grad, 10)
     if (!A.expect(type >= 0 && grad_type >= 0 && vocab >= 0 && dy->dim() >= 1 && (!accumulate || g0))) return nullptr;
     const int64_t n = t->numel(), dim = dy->size(-1);
     if (!A.expect((__int128)dy->numel() == (__int128)n * dim)) return nullptr;
-    void* st = stream_of(A, 9, *dy);
+    const CallStream st = stream_of(A, 9, *dy);
     if (!A.ok) return nullptr;
     at::Tensor g = g0 ? *g0 : new_tensor({vocab, dim}, gt, *dy, st);
     if (!A.expect((__int128)g.numel() >= (__int128)vocab * dim)) return nullptr;
