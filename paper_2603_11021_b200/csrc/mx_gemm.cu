@@ -2,6 +2,7 @@
 // Y[t][i] = sum_k X[t][k] W[i][k], both operands as llvq_mx_quantize leaves them, sums in binary32, Y in bf16.
 #include "kernels_common.cuh"
 #include "mx_tensor.cuh"
+#include "mx_tiles.h"
 
 namespace {
 
@@ -273,9 +274,10 @@ mx_gemm_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     if (warp == 1) tmem_dealloc(tmem, S::kTmem);
 }
 
-template <int kRt, int kBn>
+template <int kTile>
 int launch_mx_gemm(const llvq_ctx* ctx, const uint8_t* x_codes, const uint8_t* w_codes, int64_t k_in, MmArgs a, cudaStream_t st)
 {
+    constexpr int kRt = kMxTiles[kTile].rows / 128, kBn = kMxTiles[kTile].tokens;
     using S = MmShape<kRt, kBn>;
     CUtensorMap w_map, x_map;
     const int64_t pitch = mx_code_pitch(k_in);
@@ -306,20 +308,10 @@ extern "C" int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const
     MmArgs a{};
     a.w_scales = d_scales; a.x_scales = d_x_scales; a.n_out = n_out; a.tokens = tokens; a.kb = (uint32_t)mx_blocks(k_in); a.pitch = (uint32_t)mx_scale_pitch(k_in);
     a.k_stages = (a.kb + 7) / 8; a.y = reinterpret_cast<__nv_bfloat16*>(d_y_bf16); a.flags = ctx->dev.flags;
-    // The tile whose rounds over the SMs take least, at the cycles that a stage takes and some for the end of a tile, which writes it.  us with the four:
-    // 28672 x 8192 x 2048 tokens 221, 226, 257, 423; 8192 x 8192 x 4096 142, 135, 156, 259; 4096 x 11008 x 512 36, 26, 20, 30; 4096 x 4096 x 237 18, 12, 9.0, 8.8.
-    const struct { int rows, bn, stage, end; } shapes[4] = {{256, 224, 1450, 4500}, {128, 256, 970, 1500}, {128, 128, 560, 1000}, {128, 64, 420, 700}};
-    int pick = 0;
-    uint64_t best = ~0ull;
-    for (int i = 0; i < 4; ++i) {
-        const uint64_t tiles = (uint64_t)((n_out + shapes[i].rows - 1) / shapes[i].rows) * (uint64_t)((tokens + shapes[i].bn - 1) / shapes[i].bn);
-        const uint64_t cost = (tiles + ctx->sm_count - 1) / ctx->sm_count * ((uint64_t)a.k_stages * shapes[i].stage + shapes[i].end);
-        if (cost < best) { best = cost; pick = i; }
-    }
-    switch (pick) {
-        case 0: return launch_mx_gemm<2, 224>(ctx, d_x_codes, d_codes, k_in, a, st);
-        case 1: return launch_mx_gemm<1, 256>(ctx, d_x_codes, d_codes, k_in, a, st);
-        case 2: return launch_mx_gemm<1, 128>(ctx, d_x_codes, d_codes, k_in, a, st);
-        default: return launch_mx_gemm<1, 64>(ctx, d_x_codes, d_codes, k_in, a, st);
+    switch (mx_tile_of(n_out, tokens, a.k_stages, ctx->sm_count)) {
+        case 0: return launch_mx_gemm<0>(ctx, d_x_codes, d_codes, k_in, a, st);
+        case 1: return launch_mx_gemm<1>(ctx, d_x_codes, d_codes, k_in, a, st);
+        case 2: return launch_mx_gemm<2>(ctx, d_x_codes, d_codes, k_in, a, st);
+        default: return launch_mx_gemm<3>(ctx, d_x_codes, d_codes, k_in, a, st);
     }
 }
