@@ -433,7 +433,8 @@ int llvq_mx_dequant_matrix(const llvq_ctx* ctx, const uint8_t* d_codes, const ui
 
 /*
  * y = W x and Y[b][i] = sum_k X[b][k] W[i][k] (batch <= 64) with W (n_out x k_in) in 4 bits and bf16 activations; products are
- * accumulated in binary32, in an order that the sizes (and the device) fix.  The activations enter as binary16 or e4m3 numbers with powers of two
+ * accumulated in binary32, in an order that the sizes (and the device) fix.  An infinity or a NaN in X acts as in
+ * binary32 arithmetic (infinity times zero is NaN), on its own row alone.  The activations enter as binary16 or e4m3 numbers with powers of two
  * beside them: exact down to 2^-19 of the largest finite one of their 32 columns, off by at most 2^-27 of that one below.
  * d_x_bf16: [batch][k_in], 2-byte aligned, any k_in (rows on 16-byte boundaries are read fastest).  d_y: [n_out] float or bf16
  * bits; d_y_bf16: [batch][n_out] bf16 bits.  Sizes up to 2^30.  d_work: 256-byte aligned device memory of llvq_mx_small_batch_bytes

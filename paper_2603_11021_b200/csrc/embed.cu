@@ -607,7 +607,8 @@ int bits_of(uint64_t v)
     return b;
 }
 
-// Positions per warp of the sums: as many as leave a warp to every slot of 148 SMs with 24 each, 32 at most and 8 at least.
+// Positions per warp of the sums: as many as leave a warp to every slot of 148 SMs with 24 each, 32 at most and 8 at least.  The same on every device: the
+// order of the additions and the size of the workspace follow from it.
 int piece_of(int64_t n, int64_t dim)
 {
     int piece = 32;

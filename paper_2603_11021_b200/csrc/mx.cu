@@ -120,7 +120,7 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t rows, uint32_t cols, int64_t
 // lane the word of codes whose elements are its own in the tile) and their scales.  X: one row is brought and converted by four more warps;
 // several rows are converted once ahead by a kernel of their own and copied by one more warp, and W is read while that kernel still runs.  The stages in
 // flight are what hides the latency of HBM, which bounds the kernel for up to about 16 rows of X (4.25 bits per weight, read once: 128256 x 4096,
-// one row, 54 us, 79 % of the measured bandwidth); beyond, the products do.
+// one row, 58 us in calls back to back, 74 % of the measured bandwidth); beyond, the products do.
 constexpr int kChunk = 512;                              // columns of a warp's part of a stage
 constexpr int kXWarps = 4;
 constexpr uint32_t kXPitch = kChunk * 2 + 64;            // bytes: eight rows' 16-byte reads meet no bank twice; the exponent is behind the columns,
@@ -423,7 +423,9 @@ mx_stream_kernel(const __grid_constant__ CUtensorMap codes, const __grid_constan
                         }
                     }
                     // Scales from 2^-63 to 2^64 (bits 7 and 6 differ) and activations whose factor is not far from one: sums times scales stay well inside
-                    // binary32, and the factor is taken off once per chunk.  Else both exponents are added block by block.
+                    // binary32, and the factor is taken off once per chunk.  Else both exponents are added block by block, at half the speed or less: so for a
+                    // warp's 16 rows and 512 columns with a block of zeros (scale 0) among them (28672 x 8192 with a tenth of the blocks zero: one row of X
+                    // 56 us instead of 33, 16 rows 86 instead of 41), and where blocks of X have factors of their own (57 and 67).
                     uint32_t usual = 0x80808080u;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) usual &= (ea[j] ^ (ea[j] << 1)) & (eb[j] ^ (eb[j] << 1));

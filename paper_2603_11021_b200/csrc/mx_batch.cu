@@ -25,8 +25,9 @@ using namespace llvq;
 //               instruction takes 4-bit operands
 //   warp 16     the scales of W    warp 18: X    warp 19: the MMAs, eight per step    warps 0-7: the accumulators and Y
 // It begins to read W while the first kernel still runs (which waits for everything before it first).
-// Bound by shared memory at 64 rows of X (28672 x 8192: 54.9 us, 0.75 us or 1400 cycles a step): per step the MMAs read 80 KB (640 cycles at 128 bytes), codes
-// are written, read and spread (512, the spread ones into every other pair of banks), X is written (200).  Fewer rows of X: by that and the latency of HBM.
+// Bound by shared memory at 64 rows of X (28672 x 8192: 98 000 cycles, 1400 of them a step; 54 us at 1965 MHz, 63 in calls back to back, when the power limit
+// leaves 1665): per step the MMAs read 80 KB (640 cycles at 128 bytes), codes are written, read and spread (512, the spread ones into every other pair of
+// banks), X is written (200).  Fewer rows of X: by that and the latency of HBM.
 constexpr int kBatchRows = 256, kBatchCols = 128, kBatchThreads = 640;
 constexpr uint32_t kBatchA = kBatchRows * kBatchCols;     // bytes of a step's weights as operand, a byte of room per element
 constexpr uint32_t kBatchCode = kBatchA / 2;              // and as they are stored
@@ -180,6 +181,8 @@ __device__ __forceinline__ uint32_t nibble_tops(uint32_t bits)
 // Rows of X that hold an infinity and no NaN (bits of `rows`), which the three terms cannot hold, for one row of W per thread: infinity times what is not
 // zero is an infinity, times zero NaN, and what is finite does not matter beside it.  So signs and zeros of the codes that meet an infinity decide, 32 of
 // them at a time: one load of a row's block per thread, and the infinities of a block of X by ballot.  All lanes of the warp come here.
+// (28672 x 8192, 64 rows: 54 us without an infinity, 109 with one, 280 with nothing else; 12 ms where rows of W also have one sign and no zero, so that nothing
+// is decided before the end.)
 __device__ __noinline__ void mend_row(const BatchArgs& a, uint64_t rows, int64_t row)
 {
     const int lane = threadIdx.x & 31;
@@ -371,7 +374,8 @@ mx_batch_kernel(const __grid_constant__ CUtensorMap code_map, const __grid_const
                 ok = __all_sync(0xffffffffu, mbar_wait_copies(x_full + x.at, x.phase) && mbar_wait_copies(full + in.at, in.phase));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + (stages == 2u ? it & 1u : in.at) * 16u, tb = ta + 8u;      // a place of scales per stage
+                // scales have a place per stage; with two of them the step's number gives the same place without the ring (58.6 -> 54.9 us)
+                const uint32_t off = in.at * (kStage >> 4), x_off = x.at * x16, ta = tmem + 384u + (stages == 2u ? it & 1u : in.at) * 16u, tb = ta + 8u;
                 const uint64_t da = da0 + off, db = db0 + x_off, sa = sa0 + off, sb = sb0 + x_off;
                 if (elect_one()) {
                     scales_to_tmem(ta, sa);

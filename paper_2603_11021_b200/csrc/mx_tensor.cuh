@@ -8,8 +8,8 @@ namespace llvq {
 
 constexpr uint32_t kScaleAtom = 512;                      // scales of 128 rows and 4 blocks: row r at 16 (r % 32) + 4 (r / 32), block j at byte j
 
-// One lane of a warp whose lanes are all here.  Loops that issue MMAs are run by the whole warp and only the instructions themselves by this lane, so
-// that their operands stay in uniform registers: in a branch on the lane's number every operand is moved there for each instruction.
+// One lane of a warp whose lanes are all here.  Loops that issue MMAs are run by the whole warp and only the instructions themselves by this lane: with the
+// loop in a branch on the lane's number 28672 x 8192 took 667 us instead of 543 for 4096 tokens, and 85 instead of 64 for 64 rows.
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t is;
