@@ -458,8 +458,8 @@ int llvq_mx_gemm(const llvq_ctx* ctx, const uint8_t* d_x_codes, const uint8_t* d
 /*
  * Rows of a table by token: d_out[i][c] = scale * table[d_tokens[i]][c], one multiplication in binary32 and one rounding to the
  * output's type (bf16 for a table in 4 bits, else the table's).  d_table: [vocab][dim] of dtype; d_tokens: [n] of int32
- * (token_bytes = 4) or int64 (8); d_out: [n][dim].  All aligned to their elements.  A token outside [0, vocab) gives a row of
- * zeros and is counted like an out-of-range index (llvq_last_error).
+ * (token_bytes = 4) or int64 (8); d_out: [n][dim].  All aligned to their elements; vocab >= 1 where there is something to do.  A token
+ * outside [0, vocab) gives a row of zeros and is counted like an out-of-range index (llvq_last_error).
  */
 int llvq_embed(const llvq_ctx* ctx, const void* d_table, int dtype, int64_t vocab, int64_t dim, const void* d_tokens,
                int token_bytes, int64_t n, float scale, void* d_out, void* stream);
@@ -470,7 +470,8 @@ int llvq_mx_embed(const llvq_ctx* ctx, const uint8_t* d_codes, const uint8_t* d_
  * The gradient of llvq_embed with respect to its table: d_grad[v][c] = scale * sum of d_dy[i][c] over the i with token v (plus what
  * d_grad held, with accumulate != 0), summed in binary32 in an order that the tokens alone fix (two calls on the same inputs
  * agree to the bit), rounded once.  Tokens equal to padding_idx contribute nothing (-1: no such row; a token of -1 is then left
- * out); other tokens outside [0, vocab) contribute nothing and are counted.  Every row of d_grad is written unless accumulate is set.
+ * out); other tokens outside [0, vocab) contribute nothing and are counted (but not where vocab or dim is 0, and there is nothing
+ * to do).  Every row of d_grad is written unless accumulate is set.
  * d_dy: [n][dim] of dy_dtype; d_grad: [vocab][dim] of grad_dtype; any of the three types each.  d_work: 256-byte aligned device
  * memory of llvq_embed_grad_bytes(n, dim) bytes (0: sizes that are not supported, or nothing to do), which belongs to the call
  * until it is done: calls that may overlap need one each.

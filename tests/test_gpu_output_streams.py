@@ -127,3 +127,20 @@ def test_the_default_stream_given_while_another_is_current(calls, same):
             got = calls[name](stream=torch.cuda.default_stream())
         torch.cuda.synchronize()
         assert same(name, got, want)
+
+
+def test_captured_on_a_stream_that_forks_from_the_current_one(calls, same):
+    for name in ("mx_small_40", "mx_quantize", "embed_grad", "gemm", "sort"):
+        want, side = calls[name](), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            side.wait_stream(torch.cuda.current_stream())
+            calls[name](stream=side)                       # dropped at once
+            got = calls[name](stream=side)
+            torch.cuda.current_stream().wait_stream(side)
+            copy = got.clone()
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert same(name, got, want) and same(name, copy, want)
